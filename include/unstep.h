@@ -9,6 +9,9 @@
  *   2. unstep_rope_kv_append  rotate Q and K, write K and V into the KV ring
  *   3. unstep_window_attn     attention of the chunk's queries over the window
  *
+ * and the same with an 8-bit cache and a model's own kind of rotary positions: unstep_rotary_table,
+ * unstep_rotary_kv_append_q8, unstep_window_attn_q8, with unstep_rotary_apply and unstep_kv_read_q8 beside them.
+ *
  * Conventions
  *   - Every tensor pointer is a DEVICE pointer unless the comment says HOST.
  *   - bf16 tensors are dense, row-major, 16-byte aligned; the caller owns all of
@@ -211,6 +214,95 @@ int unstep_rmsnorm_rope_kv_append(const unstep_shape_t* shape, int32_t sink_fram
 int unstep_window_attn_noalloc(const unstep_shape_t* shape, const int32_t* start_frame,
                                int32_t window_frames, const void* q_rot, const void* ring_k,
                                const void* ring_v, void* out, void* cuda_stream);
+
+/*
+ * Rotary positions of a model: layout of the pairs, the part of the head that is rotated, and frequencies
+ * scaled for clips longer than those it was trained on.  (The paper rotates interleaved pairs of the whole head with
+ * plain frequencies; models of this kind differ in all three.)
+ *
+ * R = band_t + band_h + band_w of the shape, a multiple of 16 from 16 to 128, is the rotated part of a head; dims
+ * R .. 127 pass through.  In the calls that take an unstep_rope_t, and in those on a quantised cache, a band may be 0
+ * (one axis only: band_t = R on a grid of 1 x T).  Pair j in [0, R/2) is (x[2j], x[2j+1]), with `half` (x[j], x[j + R/2]).  Its
+ * frequency, for local pair i of the band of axis a with d_a dims, is
+ *     omega = rope_base^(-2i/d_a)
+ *     omega' = omega * (keep + (1 - keep) / factor[a]),   keep = clamp((trained[a] * omega / (2 pi) - beta_slow)
+ *                                                                      / (beta_fast - beta_slow), 0, 1)
+ * so that pairs which turn often within the `trained` positions keep their frequency and slow ones are stretched by
+ * `factor`; with trained[a] = 0 all pairs of the axis are stretched (keep = 0).
+ */
+typedef struct {
+  int32_t half;        /* 0: pairs (2j, 2j+1), 1: pairs (j, j + R/2) */
+  int32_t trained[3];  /* positions of each axis (frame, row, column) that the model was trained on, >= 0 */
+  double factor[3];    /* >= 1; 1 leaves the axis as it is */
+  double beta_slow, beta_fast;  /* turns within `trained`: 0 <= beta_slow < beta_fast */
+  double magnitude;    /* > 0: factor of cos and sin (it scales q and k, and so the scores by its square) */
+} unstep_rope_t;
+
+/*
+ * unstep_rope_table for an unstep_rope_t: cos_out, sin_out float32 [L, R/2], written with magnitude * cos and
+ * magnitude * sin of position * omega', angle, trig and product in double, rounded once.
+ */
+int unstep_rotary_table(const unstep_shape_t* shape, const unstep_rope_t* rope, int32_t start_frame, float* cos_out,
+                        float* sin_out, void* cuda_stream);
+
+/*
+ * Rotation of one tensor, without a cache: queries that attend a cache filled before, keys that are moved.  For a pair
+ * (a, b) with c = cos[n][j], s = sin[n][j]:
+ *     y_a = fl32(fl32(x_a*c) - fl32(x_b*s)),  y_b = fl32(fl32(x_a*s) + fl32(x_b*c))     (no fused multiply-add)
+ * rounded to bf16 (nearest even); dims from R on are copied bit by bit.  With `transposed`, s is negated: the transpose of the
+ * rotation, which is its backward pass (gradient of y in, gradient of x out) and, for a magnitude of 1, undoes it.
+ *   x    : bf16 [B, L, Hn, 128], read.       y : the same shape, written; may be the same buffer as x.
+ *   cos, sin, table_stream_stride : as in unstep_rope_kv_append, with rows of R/2.
+ */
+int unstep_rotary_apply(const unstep_shape_t* shape, const unstep_rope_t* rope, int32_t transposed, const void* x,
+                        const float* cos, const float* sin, int64_t table_stream_stride, void* y, void* cuda_stream);
+
+/*
+ * KV cache in 8 bits.  Every 32 neighbouring dims of a cached key or value share a power of two:
+ *     cache_k, cache_v : e4m3 codes [B, sink_frames + C, T, Hn, 128], 16-byte aligned
+ *     scale_k, scale_v : e8m0 bytes [B, sink_frames + C, T, Hn, 4], 4-byte aligned; byte E stands for 2^(E - 127)
+ * and hold code * 2^(E - 127).  Slots as in unstep_rope_kv_append_sink.  132 bytes a head instead of 256.
+ *
+ * Quantising a block of float32 values x with the largest magnitude m: E - 127 is the least integer >= -124 with
+ * m <= 448 * 2^(E - 127), the code is x * 2^-(E - 127) rounded to e4m3 (nearest even), which is off by at most 2^-4 of the value
+ * or 2^-10 * 2^(E - 127).  A block that holds a NaN, an infinity or a magnitude of 1.9375 * 2^127 or more has codes 0 and E = 255
+ * and reads as NaN throughout.  What is read is exact in bf16, for every block that was written this way.
+ */
+
+/*
+ * The append into such a cache: (RMS norm of q and k,) rotation of q and k as unstep_rotary_apply computes it, q_out rounded
+ * to bf16; the rotated k, in float32, and v are quantised and written.
+ *   gain_q, gain_k : float32 [Hn*128], 16-byte aligned, or both NULL for no norm.  The norm is
+ *                    y = x * (1 / sqrt(mean(x^2) + eps)) * gain over all Hn*128 channels of a token, in float32, and is not
+ *                    rounded to bf16 in front of the rotation (unstep_rmsnorm_rope_kv_append does round it).   eps : >= 0.
+ *   cos, sin       : float32 rows of R/2.
+ * All other arguments as in unstep_rope_kv_append_sink.
+ */
+int unstep_rotary_kv_append_q8(const unstep_shape_t* shape, const unstep_rope_t* rope, int32_t sink_frames,
+                               const int32_t* start_frame, const void* q_in, const void* k_in, const void* v_in,
+                               const float* gain_q, const float* gain_k, float eps, const float* cos, const float* sin,
+                               int64_t table_stream_stride, void* q_out, void* cache_k, void* scale_k, void* cache_v,
+                               void* scale_v, void* cuda_stream);
+
+/*
+ * Frames of such a cache read back: frames [first_frame[b], first_frame[b] + n_frames) of every stream b, in frame order, to
+ *   out_k, out_v : bf16 [B, n_frames, T, Hn, 128], written.
+ * Keys come as they were cached, rotated.
+ *   first_frame : HOST int32 [B], each >= 0.     n_frames : >= 1; at most C of the frames may lie behind the sink.
+ * Every frame must have been appended and not yet overwritten.
+ */
+int unstep_kv_read_q8(const unstep_shape_t* shape, int32_t sink_frames, const int32_t* first_frame, int32_t n_frames,
+                      const void* cache_k, const void* scale_k, const void* cache_v, const void* scale_v, void* out_k,
+                      void* out_v, void* cuda_stream);
+
+/*
+ * unstep_window_attn_sink over such a cache: the same frames, the same softmax, the keys and values as they are read back.
+ * The scratch is that of unstep_window_attn, shared with it; all it says about streams, captures and graphs holds here.
+ *   q_rot, out : bf16 [B, L, Hn, 128].
+ */
+int unstep_window_attn_q8(const unstep_shape_t* shape, int32_t sink_frames, const int32_t* start_frame,
+                          int32_t recent_frames, int32_t sink_attend, const void* q_rot, const void* cache_k,
+                          const void* scale_k, const void* cache_v, const void* scale_v, void* out, void* cuda_stream);
 
 /*
  * The work split of one unstep_window_attn(_sink) launch, listed on the host by the same integer

@@ -15,8 +15,9 @@ from . import build as _build
 EXPORTS = ("unstep_rope_table", "unstep_rope_kv_append", "unstep_window_attn",
            "unstep_window_attn_noalloc", "unstep_rope_kv_append_sink", "unstep_window_attn_sink",
            "unstep_rmsnorm_rope_kv_append", "unstep_window_attn_plan", "unstep_window_attn_plan_clusters",
-           "unstep_attn_workers", "unstep_attn_clusters", "unstep_selftest_wait_limit", "unstep_shutdown",
-           "unstep_strerror", "unstep_poll_status", "unstep_launch_count")
+           "unstep_rotary_table", "unstep_rotary_apply", "unstep_rotary_kv_append_q8", "unstep_kv_read_q8",
+           "unstep_window_attn_q8", "unstep_attn_workers", "unstep_attn_clusters", "unstep_selftest_wait_limit",
+           "unstep_shutdown", "unstep_strerror", "unstep_poll_status", "unstep_launch_count")
 
 
 class UnstepError(RuntimeError):
@@ -45,6 +46,20 @@ class Shape(ctypes.Structure):
     @property
     def chunk_tokens(self):
         return self.chunk_frames * self.grid_h * self.grid_w
+
+    @property
+    def rotated_dims(self):
+        return self.band_t + self.band_h + self.band_w
+
+
+class Rope(ctypes.Structure):
+    """Mirror of unstep_rope_t: layout and scaling of a model's rotary positions.  The axes are (frame, row, column)."""
+    _fields_ = [("half", c_int32), ("trained", c_int32 * 3), ("factor", c_double * 3), ("beta_slow", c_double),
+                ("beta_fast", c_double), ("magnitude", c_double)]
+
+    @classmethod
+    def make(cls, half=False, factor=(1.0, 1.0, 1.0), trained=(0, 0, 0), beta=(1.0, 32.0), magnitude=1.0):
+        return cls(int(half), (c_int32 * 3)(*trained), (c_double * 3)(*factor), beta[0], beta[1], magnitude)
 
 
 _lib = None
@@ -95,6 +110,19 @@ def lib() -> ctypes.CDLL:
         L.unstep_window_attn_plan_clusters.argtypes = [POINTER(Shape), c_int32, POINTER(c_int32), c_int32, c_int32,
                                                        c_int32, POINTER(c_int32), POINTER(c_int32), c_int32,
                                                        POINTER(c_int32)]
+        L.unstep_rotary_table.restype = c_int
+        L.unstep_rotary_table.argtypes = [POINTER(Shape), POINTER(Rope), c_int32, c_void_p, c_void_p, c_void_p]
+        L.unstep_rotary_apply.restype = c_int
+        L.unstep_rotary_apply.argtypes = [POINTER(Shape), POINTER(Rope), c_int32, c_void_p, c_void_p, c_void_p,
+                                          c_int64, c_void_p, c_void_p]
+        L.unstep_rotary_kv_append_q8.restype = c_int
+        L.unstep_rotary_kv_append_q8.argtypes = [POINTER(Shape), POINTER(Rope), c_int32, POINTER(c_int32)] + \
+            [c_void_p] * 5 + [c_float, c_void_p, c_void_p, c_int64] + [c_void_p] * 6
+        L.unstep_kv_read_q8.restype = c_int
+        L.unstep_kv_read_q8.argtypes = [POINTER(Shape), c_int32, POINTER(c_int32), c_int32] + [c_void_p] * 7
+        L.unstep_window_attn_q8.restype = c_int
+        L.unstep_window_attn_q8.argtypes = [POINTER(Shape), c_int32, POINTER(c_int32), c_int32, c_int32] + \
+            [c_void_p] * 7
         L.unstep_attn_clusters.restype = c_int
         L.unstep_attn_clusters.argtypes = [POINTER(c_int32)]
         L.unstep_attn_workers.restype = c_int
@@ -124,9 +152,10 @@ def _native():
             warnings.warn(f"calls are marshalled by ctypes, 8-10 us each: {e}", RuntimeWarning, stacklevel=3)
             _fast = _NoMarshal()
             return _fast
-        mod.bind(Shape, *(ctypes.cast(f, c_void_p).value for f in (
+        mod.bind(Shape, Rope, *(ctypes.cast(f, c_void_p).value for f in (
             L.unstep_rope_table, L.unstep_rope_kv_append_sink, L.unstep_rmsnorm_rope_kv_append,
-            L.unstep_window_attn, L.unstep_window_attn_noalloc, L.unstep_window_attn_sink)))
+            L.unstep_window_attn, L.unstep_window_attn_noalloc, L.unstep_window_attn_sink, L.unstep_rotary_table,
+            L.unstep_rotary_apply, L.unstep_rotary_kv_append_q8, L.unstep_kv_read_q8, L.unstep_window_attn_q8)))
         _fast = mod
     return _fast
 
@@ -150,6 +179,15 @@ def _dev_ptr(t, dtype, numel, name):
         raise ValueError(f"{name}: expected contiguous {dtype} with {numel} elements, got "
                          f"{t.dtype} {tuple(t.shape)}")
     return c_void_p(t.data_ptr())
+
+
+def _here_ptr(t, dtype, numel, name):
+    """_dev_ptr of a tensor on the current device, where the call is enqueued."""
+    import torch
+    ptr = _dev_ptr(t, dtype, numel, name)
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name}: on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    return ptr
 
 
 def _starts(shape: Shape, start_frame):
@@ -346,6 +384,145 @@ def _general_window_attn_sink(shape, sink_frames, start_frame, recent_frames, si
         int(sink_attend), _dev_ptr(q_rot, bf, n, "q_rot"), _dev_ptr(cache_k, bf, nr, "cache_k"),
         _dev_ptr(cache_v, bf, nr, "cache_v"), _dev_ptr(out, bf, n, "out"), _stream_ptr(stream)),
         "unstep_window_attn_sink")
+
+
+def rotary_table(shape: Shape, rope: Rope, start_frame: int, cos, sin, stream=None):
+    """unstep_rotary_table: fill float32 cos/sin [L, R/2] for the chunk starting at start_frame, R the dims that the
+    bands of the shape rotate."""
+    rc = (_fast or _native()).rotary_table(shape, rope, start_frame, cos, sin, stream)
+    if rc is None:
+        _general_rotary_table(shape, rope, start_frame, cos, sin, stream)
+    elif rc:
+        raise UnstepError(rc, "unstep_rotary_table")
+
+
+def _rope(rope):
+    if not isinstance(rope, Rope):
+        raise TypeError("rope: expected a Rope")
+    return ctypes.byref(rope)
+
+
+def _general_rotary_table(shape, rope, start_frame, cos, sin, stream):
+    import torch
+    n = shape.chunk_tokens * (shape.rotated_dims // 2)
+    _check(lib().unstep_rotary_table(ctypes.byref(shape), _rope(rope), int(start_frame),
+                                     _here_ptr(cos, torch.float32, n, "cos"),
+                                     _here_ptr(sin, torch.float32, n, "sin"), _stream_ptr(stream)),
+           "unstep_rotary_table")
+
+
+def _rotary_table_numel(shape, table_stream_stride):
+    return shape.chunk_tokens * (shape.rotated_dims // 2) + (shape.batch - 1) * int(table_stream_stride)
+
+
+def rotary_apply(shape: Shape, rope: Rope, x, cos, sin, y, transposed: bool = False, table_stream_stride: int = 0,
+                 stream=None):
+    """unstep_rotary_apply: rotate x [B, L, Hn, 128] into y; transposed: its backward pass."""
+    rc = (_fast or _native()).rotary_apply(shape, rope, x, cos, sin, y, transposed, table_stream_stride, stream)
+    if rc is None:
+        _general_rotary_apply(shape, rope, x, cos, sin, y, transposed, table_stream_stride, stream)
+    elif rc:
+        raise UnstepError(rc, "unstep_rotary_apply")
+
+
+def _general_rotary_apply(shape, rope, x, cos, sin, y, transposed, table_stream_stride, stream):
+    import torch
+    n = shape.batch * shape.chunk_tokens * shape.heads * shape.head_dim
+    ntab = _rotary_table_numel(shape, table_stream_stride)
+    _check(lib().unstep_rotary_apply(
+        ctypes.byref(shape), _rope(rope), int(bool(transposed)), _here_ptr(x, torch.bfloat16, n, "x"),
+        _here_ptr(cos, torch.float32, ntab, "cos"), _here_ptr(sin, torch.float32, ntab, "sin"),
+        int(table_stream_stride), _here_ptr(y, torch.bfloat16, n, "y"), _stream_ptr(stream)), "unstep_rotary_apply")
+
+
+def _cache8_ptrs(shape, sink_frames, cache_k, scale_k, cache_v, scale_v):
+    import torch
+    n = (shape.batch * (shape.ring_frames + int(sink_frames)) * shape.tokens_per_frame * shape.heads
+         * shape.head_dim)
+    codes, scales = torch.float8_e4m3fn, torch.float8_e8m0fnu
+    return (_here_ptr(cache_k, codes, n, "cache_k"), _here_ptr(scale_k, scales, n // 32, "scale_k"),
+            _here_ptr(cache_v, codes, n, "cache_v"), _here_ptr(scale_v, scales, n // 32, "scale_v"))
+
+
+def rotary_kv_append_q8(shape: Shape, rope: Rope, sink_frames: int, start_frame, q_in, k_in, v_in, cos, sin, q_out,
+                        cache_k, scale_k, cache_v, scale_v, gain_q=None, gain_k=None, eps: float = 0.0,
+                        table_stream_stride: int = 0, stream=None):
+    """unstep_rotary_kv_append_q8: (RMSNorm and) rotation of q and k, k and v quantised into the cache.  cache_k,
+    cache_v: float8_e4m3fn [B, sink + C, T, Hn, 128], scale_k, scale_v: float8_e8m0fnu [B, sink + C, T, Hn, 4]."""
+    rc = (_fast or _native()).append_q8(
+        shape, rope, sink_frames, start_frame, q_in, k_in, v_in, cos, sin, q_out, cache_k, scale_k, cache_v, scale_v,
+        gain_q, gain_k, eps, table_stream_stride, stream)
+    if rc is None:
+        _general_rotary_kv_append_q8(shape, rope, sink_frames, start_frame, q_in, k_in, v_in, cos, sin, q_out, cache_k,
+                                     scale_k, cache_v, scale_v, gain_q, gain_k, eps, table_stream_stride, stream)
+    elif rc:
+        raise UnstepError(rc, "unstep_rotary_kv_append_q8")
+
+
+def _general_rotary_kv_append_q8(shape, rope, sink_frames, start_frame, q_in, k_in, v_in, cos, sin, q_out, cache_k,
+                                 scale_k, cache_v, scale_v, gain_q, gain_k, eps, table_stream_stride, stream):
+    import torch
+    bf = torch.bfloat16
+    n = shape.batch * shape.chunk_tokens * shape.heads * shape.head_dim
+    ntab = _rotary_table_numel(shape, table_stream_stride)
+    ng = shape.heads * shape.head_dim
+    gains = [None if g is None else _here_ptr(g, torch.float32, ng, name)
+             for g, name in ((gain_q, "gain_q"), (gain_k, "gain_k"))]
+    _check(lib().unstep_rotary_kv_append_q8(
+        ctypes.byref(shape), _rope(rope), int(sink_frames), _starts(shape, start_frame),
+        _here_ptr(q_in, bf, n, "q_in"), _here_ptr(k_in, bf, n, "k_in"), _here_ptr(v_in, bf, n, "v_in"), *gains,
+        c_float(eps), _here_ptr(cos, torch.float32, ntab, "cos"), _here_ptr(sin, torch.float32, ntab, "sin"),
+        int(table_stream_stride), _here_ptr(q_out, bf, n, "q_out"),
+        *_cache8_ptrs(shape, sink_frames, cache_k, scale_k, cache_v, scale_v), _stream_ptr(stream)),
+        "unstep_rotary_kv_append_q8")
+
+
+def kv_read_q8(shape: Shape, sink_frames: int, first_frame, n_frames: int, cache_k, scale_k, cache_v, scale_v, out_k,
+               out_v, stream=None):
+    """unstep_kv_read_q8: frames [first_frame[b], first_frame[b] + n_frames) of an 8-bit cache as bf16
+    [B, n_frames, T, Hn, 128]."""
+    rc = (_fast or _native()).read_q8(
+        shape, sink_frames, first_frame, n_frames, cache_k, scale_k, cache_v, scale_v, out_k, out_v, stream)
+    if rc is None:
+        _general_kv_read_q8(shape, sink_frames, first_frame, n_frames, cache_k, scale_k, cache_v, scale_v, out_k, out_v,
+                            stream)
+    elif rc:
+        raise UnstepError(rc, "unstep_kv_read_q8")
+
+
+def _general_kv_read_q8(shape, sink_frames, first_frame, n_frames, cache_k, scale_k, cache_v, scale_v, out_k, out_v,
+                        stream):
+    import torch
+    n = shape.batch * int(n_frames) * shape.tokens_per_frame * shape.heads * shape.head_dim
+    _check(lib().unstep_kv_read_q8(
+        ctypes.byref(shape), int(sink_frames), _starts(shape, first_frame), int(n_frames),
+        *_cache8_ptrs(shape, sink_frames, cache_k, scale_k, cache_v, scale_v),
+        _here_ptr(out_k, torch.bfloat16, n, "out_k"), _here_ptr(out_v, torch.bfloat16, n, "out_v"),
+        _stream_ptr(stream)), "unstep_kv_read_q8")
+
+
+def window_attn_q8(shape: Shape, sink_frames: int, start_frame, recent_frames: int, sink_attend: int, q_rot, cache_k,
+                   scale_k, cache_v, scale_v, out, stream=None):
+    """unstep_window_attn_q8: attention over sink frames + the recent window of an 8-bit cache."""
+    rc = (_fast or _native()).attn_q8(
+        shape, sink_frames, start_frame, recent_frames, sink_attend, q_rot, cache_k, scale_k, cache_v, scale_v, out,
+        stream)
+    if rc is None:
+        _general_window_attn_q8(shape, sink_frames, start_frame, recent_frames, sink_attend, q_rot, cache_k, scale_k,
+                                cache_v, scale_v, out, stream)
+    elif rc:
+        raise UnstepError(rc, "unstep_window_attn_q8")
+
+
+def _general_window_attn_q8(shape, sink_frames, start_frame, recent_frames, sink_attend, q_rot, cache_k, scale_k,
+                            cache_v, scale_v, out, stream):
+    import torch
+    bf = torch.bfloat16
+    n = shape.batch * shape.chunk_tokens * shape.heads * shape.head_dim
+    _check(lib().unstep_window_attn_q8(
+        ctypes.byref(shape), int(sink_frames), _starts(shape, start_frame), int(recent_frames), int(sink_attend),
+        _here_ptr(q_rot, bf, n, "q_rot"), *_cache8_ptrs(shape, sink_frames, cache_k, scale_k, cache_v, scale_v),
+        _here_ptr(out, bf, n, "out"), _stream_ptr(stream)), "unstep_window_attn_q8")
 
 
 def window_attn_plan(shape: Shape, start_frame, recent_frames: int, max_workers: int, sink_frames: int = 0,

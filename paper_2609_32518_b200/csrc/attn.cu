@@ -36,6 +36,7 @@
 
 #include "common.h"
 #include "ptx.cuh"
+#include "quant.cuh"
 #include "attn_sched.h"
 #include "handover.h"
 
@@ -77,15 +78,23 @@ __device__ __forceinline__ unsigned long long gtime() {
 
 constexpr int kHalfBytes = 128 * 64 * 2;    // one TMA box: 128 rows x 64 bf16 (128-byte rows)
 constexpr int kTileBytes = 2 * kHalfBytes;  // 128 x 128 bf16
-constexpr int kStages = 5;                  // 32 KB buffers shared by the K and V tiles
-constexpr int kThreads = 384;
+// What the kernel over a bf16 cache and the one over an 8-bit cache have of their own.  The latter has four more
+// warps, which decode the tiles that TMA brings as codes (kRawStages buffers) into the bf16 buffers that the other has TMA fill.
+constexpr int kRawStages = 2, kRawBytes = 128 * 128;
+template <bool kQ8>
+struct Form {
+  static constexpr int kStages = kQ8 ? 4 : 5;       // 32 KB buffers shared by the K and V tiles
+  static constexpr int kThreads = kQ8 ? 512 : 384;
+};
 constexpr int kTmemCols = 512;
 constexpr int kTmemS = 0, kTmemP = 128, kTmemO = 256;   // S (128 columns) | P0 | P1 (64 each) | O0 | O1 (128 each)
 constexpr long long kWaitCycles = 2000000000LL;  // about a second: then give up, never hang
 
 constexpr int kSmemQ = 0;
 constexpr int kSmemKV = 2 * kTileBytes;
-constexpr int kSmemBar = kSmemKV + kStages * kTileBytes;
+constexpr int kSmemRaw = kSmemKV + Form<true>::kStages * kTileBytes;
+constexpr int kSmemBar = kSmemKV + Form<false>::kStages * kTileBytes;
+static_assert(kSmemRaw + kRawStages * kRawBytes == kSmemBar, "both forms have their barriers behind their buffers");
 constexpr int kAttnSmemBytes = kSmemBar + 256;
 
 // Partial result of one query tile of a split item: O as [col / 4][row][col % 4] (unnormalised,
@@ -125,11 +134,24 @@ struct Waiter {
 
 // The CTA owns 384 x 168 registers; 128 x 72 for the service warps + 256 x 216 for the softmax
 // warps uses exactly that (an increase that the pool cannot satisfy would wait forever).  Nothing spills.
+// Over an 8-bit cache 512 x 128: 128 x 56 + 128 x 40 for the decoders + 256 x 208.
 constexpr int kRegsService = 72, kRegsSoftmax = 216;
 static_assert(128 * kRegsService + 256 * kRegsSoftmax <= 384 * 168, "register redistribution exceeds the CTA's allocation");
 static_assert(kRegsService == 72 && kRegsSoftmax == 216, "keep the setmaxnreg literals below in step");
-__device__ __forceinline__ void reg_dealloc_service() { asm volatile("setmaxnreg.dec.sync.aligned.u32 72;"); }
-__device__ __forceinline__ void reg_alloc_softmax() { asm volatile("setmaxnreg.inc.sync.aligned.u32 216;"); }
+constexpr int kRegsService8 = 56, kRegsDecode8 = 40, kRegsSoftmax8 = 208;
+static_assert(128 * kRegsService8 + 128 * kRegsDecode8 + 256 * kRegsSoftmax8 <= 512 * 128, "register redistribution exceeds the CTA's allocation");
+static_assert(kRegsService8 == 56 && kRegsDecode8 == 40 && kRegsSoftmax8 == 208, "keep the setmaxnreg literals below in step");
+template <bool kQ8>
+__device__ __forceinline__ void reg_dealloc_service() {
+  if constexpr (kQ8) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+  else asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+}
+__device__ __forceinline__ void reg_dealloc_decode() { asm volatile("setmaxnreg.dec.sync.aligned.u32 40;"); }
+template <bool kQ8>
+__device__ __forceinline__ void reg_alloc_softmax() {
+  if constexpr (kQ8) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+  else asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+}
 
 // --------------------------------------------------------------------------------------
 // Softmax of one 128 x 128 score tile with one thread per query row (a warpgroup per query
@@ -314,17 +336,40 @@ struct ValidKeys {
 // [tile][col / 4][row][col % 4], then (m, l) as [tile][row].
 constexpr int kSwapTileBytes = 128 * 128 * 4;
 constexpr int kSwapMl = 2 * kSwapTileBytes;
-static_assert(kSwapMl + 2 * 128 * 8 <= kStages * kTileBytes, "the exchange does not fit the K and V stages");
+static_assert(kSwapMl + 2 * 128 * 8 <= kSmemBar - kSmemKV, "the exchange does not fit the K and V stages");
+
+// One row (key) of a K or V tile, codes to bf16: 128 codes at `src`, TMA's 128-byte swizzle by the row, to the two
+// 64-column halves of the tile at `dst` with the same swizzle.  Eight neighbouring lanes touch different banks both
+// ways.  `word`: the row's four scale bytes.
+template <bool kTwoFactors>
+__device__ __forceinline__ void decode_row(uint32_t src, uint32_t dst, uint32_t word, uint32_t swizzle) {
+#pragma unroll 1
+  for (int block = 0; block < 4; ++block) {
+    const uint32_t byte = word & 255u, f1 = q8::factor1(byte);
+    word >>= 8;
+    const uint4 x0 = ld_shared_16(src + (((2 * block) ^ swizzle) << 4)), x1 = ld_shared_16(src + (((2 * block + 1) ^ swizzle) << 4));
+    uint4 y[4] = {q8::decode8(x0.x, x0.y, f1), q8::decode8(x0.z, x0.w, f1), q8::decode8(x1.x, x1.y, f1), q8::decode8(x1.z, x1.w, f1)};
+    const uint32_t to = dst + (block >> 1) * kHalfBytes;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (kTwoFactors) y[i] = q8::mul8(y[i], q8::factor2(byte));
+      st_shared_16(to + (((4 * (block & 1) + i) ^ swizzle) << 4), reinterpret_cast<const uint32_t*>(&y[i]));
+    }
+  }
+}
 
 // kCluster: a launch of one part per block, in which the parts of an item are a cluster and merge through each
 // other's shared memory.  The other form merges through global memory, where a part's stores, the fence
 // with its count and the last part's loads took 5-10 us one after the other.
-template <bool kCluster>
-__global__ void __launch_bounds__(kThreads, 1)
+// kQ8: over an 8-bit cache.  tm_kf and tm_vf are maps over codes then, and tm_k and tm_v are not used: the decoders write
+// all rows of a tile, so that a ragged one needs no zero fill, and frames of any length lie in runs of keys.
+template <bool kCluster, bool kQ8>
+__global__ void __launch_bounds__(Form<kQ8>::kThreads, 1)
 window_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                    const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_kf,
                    const __grid_constant__ CUtensorMap tm_vf, const AttnParams p,
                    __nv_bfloat16* __restrict__ out) {
+  constexpr int kStages = Form<kQ8>::kStages;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   const uint32_t smem_base = smem_u32(smem_raw);
   if (smem_base & 1023u) {  // the 128-byte swizzle needs 1024-byte aligned tiles
@@ -338,10 +383,12 @@ window_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   // mbarriers (8 bytes each)
   const uint32_t bar_q_full = sBar;                          // [2]  TMA -> Q K^T issuer
   const uint32_t bar_q_empty = sBar + 16;                    // [2]  Q K^T issuer -> TMA
-  const uint32_t bar_kv_full = sBar + 32;                    // [kStages] TMA -> the issuer that reads the stage
+  const uint32_t bar_kv_full = sBar + 32;                    // [kStages] TMA (kQ8: decoders) -> the issuer that reads the stage
   const uint32_t bar_kv_empty = sBar + 32 + 8 * kStages;     // [kStages] that issuer -> TMA
   const uint32_t bar_s_full = sBar + 32 + 16 * kStages;      // [2]  Q K^T issuer -> softmax a
   const uint32_t bar_pv_done = bar_s_full + 16;              // [2]  P V issuer -> softmax a
+  const uint32_t bar_raw_full = bar_pv_done + 16;            // kQ8: [kRawStages] TMA -> decoders
+  const uint32_t bar_raw_empty = bar_raw_full + 8 * kRawStages;   // kQ8: [kRawStages] decoders -> TMA
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen + kSmemBar + 224);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(gen + kSmemBar + 228);
 
@@ -358,8 +405,12 @@ window_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       mbar_init(bar_pv_done + 8 * i, 1);
     }
     for (int i = 0; i < kStages; ++i) {
-      mbar_init(bar_kv_full + 8 * i, 1);
+      mbar_init(bar_kv_full + 8 * i, kQ8 ? 4 : 1);
       mbar_init(bar_kv_empty + 8 * i, 1);
+    }
+    for (int i = 0; kQ8 && i < kRawStages; ++i) {
+      mbar_init(bar_raw_full + 8 * i, 1);
+      mbar_init(bar_raw_empty + 8 * i, 4);
     }
     *abort_flag = 0;
     mbar_fence_init();
@@ -376,8 +427,47 @@ window_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   // there, so that no bounded wait counts that kernel's time.
   const Waiter w{abort_flag, kWaitCycles};
 
-  if (warp >= 8) {
-    reg_dealloc_service();
+  if (kQ8 && warp >= 12) {
+    // ---------------------------------------------------------------- decoders
+    // A thread has a row (key) of every tile.  Its scale word comes straight from global memory, a tile ahead.
+    reg_dealloc_decode();
+    grid_wait();
+    Sched sched(p, static_cast<int>(blockIdx.x));
+    Seg s;
+    const int row = tid - 384;
+    const uint32_t swizzle = row & 7;
+    uint32_t it = 0;
+    bool ok = true;
+    while (ok && sched.next(s)) {
+      const int n = 2 * (s.t1 - s.t0);
+      auto word_of = [&](int i) {   // the i-th of the item's K and V tiles, in the order in which they come
+        const bool is_v = i > 0 && ((i & 1) == 0 || i == n - 1);
+        const TileInfo ti = tile_info(p, s.b, s.t0 + (i == n - 1 ? n / 2 - 1 : is_v ? i / 2 - 1 : (i + 1) / 2));
+        if (row >= ti.valid) return 0u;   // nobody attends it: any finite value will do
+        return ld_global_4((is_v ? p.scale_v : p.scale_k) + (s.b * p.cache_rows + ti.row + row) * p.Hn + s.h);
+      };
+      uint32_t ahead = word_of(0);
+#pragma unroll 1
+      for (int i = 0; i < n; ++i, ++it) {
+        const uint32_t word = ahead;
+        if (i + 1 < n) ahead = word_of(i + 1);
+        const uint32_t raw = it % kRawStages, st = it % kStages;
+        ok = w.wait_warp(bar_raw_full + 8 * raw, (it / kRawStages) & 1);
+        if (ok) ok = w.wait_warp(bar_kv_empty + 8 * st, ((it / kStages) & 1) ^ 1);
+        if (!ok) break;
+        const uint32_t src = smem_base + kSmemRaw + raw * kRawBytes + row * 128, dst = sKV + st * kTileBytes + row * 128;
+        if (__all_sync(0xFFFFFFFFu, __vcmpgtu4(word, 0x86868686u) == 0u)) decode_row<false>(src, dst, word, swizzle);
+        else decode_row<true>(src, dst, word, swizzle);
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(bar_kv_full + 8 * st);
+          mbar_arrive(bar_raw_empty + 8 * raw);
+        }
+      }
+    }
+  } else if (warp >= 8) {
+    reg_dealloc_service<kQ8>();
     if (warp == 10 && lane == 0) {
       // ------------------------------------------------------------ TMA producer
       prefetch_tensormap(&tm_q);
@@ -403,6 +493,15 @@ window_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
           ++q_it[a];
         };
         auto load_kv = [&](const TileInfo& ti, int kv) {
+          if constexpr (kQ8) {
+            const uint32_t raw = kv_it % kRawStages, bar = bar_raw_full + 8 * raw;
+            if (ok) ok = w.wait(bar_raw_empty + 8 * raw, ((kv_it / kRawStages) & 1) ^ 1);
+            if (!ok) return;
+            mbar_expect_tx(bar, kRawBytes);
+            tma_load_4d(smem_base + kSmemRaw + raw * kRawBytes, kv == 0 ? &tm_kf : &tm_vf, bar, 0, s.h, ti.row, s.b);
+            ++kv_it;
+            return;
+          }
           const uint32_t st = kv_it % kStages;
           if (ok) ok = w.wait(bar_kv_empty + 8 * st, ((kv_it / kStages) & 1) ^ 1);
           if (!ok) return;
@@ -532,7 +631,7 @@ window_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     // ---------------------------------------------------------------- softmax warpgroups
     // Warps 0-3 own query tile 0, warps 4-7 query tile 1; a thread owns a row from the scores
     // to the output.
-    reg_alloc_softmax();
+    reg_alloc_softmax<kQ8>();
     grid_wait();
     const int a = warp >> 2;               // query tile of this warpgroup
     const int row = tid & 127;             // row inside the tile = TMEM lane
@@ -889,9 +988,9 @@ static EncodeTiledFn get_encode_fn() {
   return fn;
 }
 
-// bf16 tensor map with 128-byte swizzle, box = 64 elements x 128 rows of dimension `row_dim`.
+// bf16 (or code) tensor map with 128-byte swizzle, box = 64 (128) elements x 128 rows of dimension `row_dim`.
 static bool make_map(CUtensorMap* m, const void* base, int rank, const uint64_t* dims,
-                     const uint64_t* strides_bytes, int row_dim) {
+                     const uint64_t* strides_bytes, int row_dim, bool codes = false) {
   EncodeTiledFn fn = get_encode_fn();
   if (fn == nullptr) return false;
   cuuint64_t gdim[5], gstride[4];
@@ -902,9 +1001,9 @@ static bool make_map(CUtensorMap* m, const void* base, int rank, const uint64_t*
     estr[i] = 1;
     if (i > 0) gstride[i - 1] = strides_bytes[i - 1];
   }
-  box[0] = 64;
+  box[0] = codes ? 128 : 64;
   box[row_dim] = 128;
-  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), gdim, gstride, box, estr,
+  return fn(m, codes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), gdim, gstride, box, estr,
             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -912,8 +1011,32 @@ static bool make_map(CUtensorMap* m, const void* base, int rank, const uint64_t*
 struct DeviceInfo {
   bool ok = false;
   int sm_count = 0;
-  int32_t clusters[kMaxClusterParts + 1] = {};   // clusters of that many blocks which the device runs at the same time
+  int32_t clusters[2][kMaxClusterParts + 1] = {};   // clusters of that many blocks which the device runs at the same
+                                                    // time, of the kernel over a bf16 and of that over an 8-bit cache
 };
+
+template <bool kQ8>
+static bool query_kernels(int32_t* clusters) {
+  if (cudaFuncSetAttribute(window_attn_kernel<false, kQ8>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttnSmemBytes) != cudaSuccess ||
+      cudaFuncSetAttribute(window_attn_kernel<true, kQ8>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttnSmemBytes) != cudaSuccess)
+    return false;
+  for (int parts = 2; parts <= kMaxClusterParts; ++parts) {
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = parts;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(parts);
+    cfg.blockDim = dim3(Form<kQ8>::kThreads);
+    cfg.dynamicSmemBytes = kAttnSmemBytes;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, window_attn_kernel<true, kQ8>, &cfg) == cudaSuccess) clusters[parts] = n;
+    else cudaGetLastError();   // no clusters of that size, then
+  }
+  return true;
+}
 
 // Set up and queried once per device and process; each thread keeps a copy for the device it uses.
 static DeviceInfo query_device(int dev) {
@@ -924,26 +1047,8 @@ static DeviceInfo query_device(int dev) {
   if (it != known.end()) return it->second;
   DeviceInfo info;
   info.ok = cudaDeviceGetAttribute(&info.sm_count, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess &&
-            cudaFuncSetAttribute(window_attn_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 kAttnSmemBytes) == cudaSuccess &&
-            cudaFuncSetAttribute(window_attn_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 kAttnSmemBytes) == cudaSuccess;
+            query_kernels<false>(info.clusters[0]) && query_kernels<true>(info.clusters[1]);
   if (!info.ok) return info;
-  for (int parts = 2; parts <= kMaxClusterParts; ++parts) {
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = parts;
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(parts);
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = kAttnSmemBytes;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, window_attn_kernel<true>, &cfg) == cudaSuccess) info.clusters[parts] = n;
-    else cudaGetLastError();   // no clusters of that size, then
-  }
   return known[dev] = info;
 }
 
@@ -1057,11 +1162,14 @@ constexpr int kOverlapSteps = 64;   // key-tile steps per worker below which a l
 // Validation, work split, tensor maps and launch shared by the attention entry points.
 // The cache has `sink_frames` slots in front of the ring (0 for the plain rolling window);
 // stream b attends frames [0, min(sink_attend, lo)) and [lo, hi), lo = max(0, hi - window_frames).
+// With `scale_k` and `scale_v` the cache is one of 8 bits.
 static int window_attn_run(const unstep_shape_t* shape, const int32_t* start_frame,
                            int32_t window_frames, const void* q_rot, const void* ring_k,
                            const void* ring_v, void* out, void* cuda_stream, ScratchFn scratch,
-                           int32_t sink_frames = 0, int32_t sink_attend = 0) {
-  int rc = check_attn_args(shape, start_frame, window_frames, sink_frames, sink_attend);
+                           int32_t sink_frames = 0, int32_t sink_attend = 0, const void* scale_k = nullptr,
+                           const void* scale_v = nullptr) {
+  const bool q8 = scale_k != nullptr;
+  int rc = check_attn_args(shape, start_frame, window_frames, sink_frames, sink_attend, q8);
   if (rc != UNSTEP_OK) return rc;
   const void* ptrs[] = {q_rot, ring_k, ring_v, out};
   for (const void* ptr : ptrs)
@@ -1075,15 +1183,17 @@ static int window_attn_run(const unstep_shape_t* shape, const int32_t* start_fra
   const uint64_t C = static_cast<uint64_t>(shape->ring_frames) + sink_frames;  // cache slots per stream
   const uint64_t T = static_cast<uint64_t>(shape->grid_h) * shape->grid_w;
   const uint64_t L = T * shape->chunk_frames;
-  const uint64_t row_bytes = Hn * kHeadDim * 2;
+  const uint64_t row_bytes = Hn * kHeadDim * 2, cache_row_bytes = q8 ? Hn * kHeadDim : row_bytes;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
 
   AttnParams p;
   plan_shape(p, shape, sink_frames);
+  if (q8) p.flat = 1;
+  p.cache_rows = static_cast<int64_t>(C * T);
   for (int b0 = 0; b0 < shape->batch; b0 += kMaxStreamsPerLaunch) {
     const int nb = shape->batch - b0 < kMaxStreamsPerLaunch ? shape->batch - b0 : kMaxStreamsPerLaunch;
     rc = plan_launch(p, shape, start_frame + b0, nb, window_frames, sink_frames, sink_attend, info.sm_count,
-                     info.clusters);
+                     info.clusters[q8]);
     if (rc != UNSTEP_OK) return rc;
     Workspace ws;
     rc = scratch(st, 2 * static_cast<size_t>(info.sm_count), 2 * static_cast<size_t>(nb) * p.items_per_stream, &ws);
@@ -1096,8 +1206,10 @@ static int window_attn_run(const unstep_shape_t* shape, const int32_t* start_fra
     p.extent_part = static_cast<int64_t>(ws.slots) * kPartFloats;
     p.extent_counters = static_cast<int64_t>(ws.n_counters);
     const char* qb = static_cast<const char*>(q_rot) + static_cast<uint64_t>(b0) * L * row_bytes;
-    const char* kb = static_cast<const char*>(ring_k) + static_cast<uint64_t>(b0) * C * T * row_bytes;
-    const char* vb = static_cast<const char*>(ring_v) + static_cast<uint64_t>(b0) * C * T * row_bytes;
+    const char* kb = static_cast<const char*>(ring_k) + static_cast<uint64_t>(b0) * C * T * cache_row_bytes;
+    const char* vb = static_cast<const char*>(ring_v) + static_cast<uint64_t>(b0) * C * T * cache_row_bytes;
+    p.scale_k = static_cast<const uint32_t*>(scale_k) + (q8 ? b0 * p.cache_rows * p.Hn : 0);
+    p.scale_v = static_cast<const uint32_t*>(scale_v) + (q8 ? b0 * p.cache_rows * p.Hn : 0);
     __nv_bfloat16* ob = reinterpret_cast<__nv_bfloat16*>(static_cast<char*>(out) +
                                                          static_cast<uint64_t>(b0) * L * row_bytes);
     CUtensorMap tm_q, tm_k, tm_v, tm_kf, tm_vf;
@@ -1106,11 +1218,16 @@ static int window_attn_run(const unstep_shape_t* shape, const int32_t* start_fra
     const uint64_t rdims[5] = {kHeadDim, Hn, T, C, static_cast<uint64_t>(nb)};
     const uint64_t rstr[4] = {kHeadDim * 2, row_bytes, T * row_bytes, C * T * row_bytes};
     const uint64_t fdims[4] = {kHeadDim, Hn, C * T, static_cast<uint64_t>(nb)};   // ring rows, flat
-    const uint64_t fstr[3] = {kHeadDim * 2, row_bytes, C * T * row_bytes};
-    if (!make_map(&tm_q, qb, 4, qdims, qstr, 2) || !make_map(&tm_k, kb, 5, rdims, rstr, 2) ||
-        !make_map(&tm_v, vb, 5, rdims, rstr, 2) || !make_map(&tm_kf, kb, 4, fdims, fstr, 2) ||
-        !make_map(&tm_vf, vb, 4, fdims, fstr, 2))
+    const uint64_t fstr[3] = {cache_row_bytes / Hn, cache_row_bytes, C * T * cache_row_bytes};
+    if (!make_map(&tm_q, qb, 4, qdims, qstr, 2) || !make_map(&tm_kf, kb, 4, fdims, fstr, 2, q8) ||
+        !make_map(&tm_vf, vb, 4, fdims, fstr, 2, q8))
       return UNSTEP_ERR_CUDA;
+    if (q8) {
+      tm_k = tm_kf;
+      tm_v = tm_vf;
+    } else if (!make_map(&tm_k, kb, 5, rdims, rstr, 2) || !make_map(&tm_v, vb, 5, rdims, rstr, 2)) {
+      return UNSTEP_ERR_CUDA;
+    }
     // Set up under the append before it where the launch is short.  Append and attention (with the pipeline of one
     // S per query tile, 10 % slower per step), us not
     // overlapped -> overlapped, by steps per worker: in runs of 20 (full clock) 24: 78.9 -> 76.5, 35:
@@ -1122,8 +1239,11 @@ static int window_attn_run(const unstep_shape_t* shape, const int32_t* start_fra
     // come down to the loss of runs at the cap (0.4 %).
     const bool brief = p.all_steps < static_cast<int64_t>(kOverlapSteps) * p.n_workers;
     const cudaError_t err =
-        launch_clusters(brief, p.cluster ? p.parts : 1, p.cluster ? window_attn_kernel<true> : window_attn_kernel<false>,
-                        p.n_workers, kThreads, kAttnSmemBytes, st, tm_q, tm_k, tm_v, tm_kf, tm_vf, p, ob);
+        launch_clusters(brief, p.cluster ? p.parts : 1,
+                        q8 ? (p.cluster ? window_attn_kernel<true, true> : window_attn_kernel<false, true>)
+                           : (p.cluster ? window_attn_kernel<true, false> : window_attn_kernel<false, false>),
+                        p.n_workers, q8 ? Form<true>::kThreads : Form<false>::kThreads, kAttnSmemBytes, st, tm_q, tm_k, tm_v,
+                        tm_kf, tm_vf, p, ob);
     g_launches.fetch_add(1);
     if (err != cudaSuccess) return UNSTEP_ERR_CUDA;
   }
@@ -1156,6 +1276,17 @@ extern "C" int unstep_window_attn_sink(const unstep_shape_t* shape, int32_t sink
                                        const void* cache_v, void* out, void* cuda_stream) {
   return window_attn_run(shape, start_frame, recent_frames, q_rot, cache_k, cache_v, out, cuda_stream,
                          get_workspace, sink_frames, sink_attend);
+}
+
+extern "C" int unstep_window_attn_q8(const unstep_shape_t* shape, int32_t sink_frames, const int32_t* start_frame,
+                                     int32_t recent_frames, int32_t sink_attend, const void* q_rot, const void* cache_k,
+                                     const void* scale_k, const void* cache_v, const void* scale_v, void* out,
+                                     void* cuda_stream) {
+  if (scale_k == nullptr || scale_v == nullptr || (reinterpret_cast<uintptr_t>(scale_k) & 3u) != 0 ||
+      (reinterpret_cast<uintptr_t>(scale_v) & 3u) != 0)
+    return UNSTEP_ERR_INVALID_ARG;
+  return window_attn_run(shape, start_frame, recent_frames, q_rot, cache_k, cache_v, out, cuda_stream,
+                         get_workspace, sink_frames, sink_attend, scale_k, scale_v);
 }
 
 // --------------------------------------------------------------------------
@@ -1243,7 +1374,7 @@ extern "C" int unstep_attn_clusters(int32_t* clusters) {
   if (rc != UNSTEP_OK) return rc;
   const DeviceInfo& info = device_info();
   if (!info.ok) return UNSTEP_ERR_CUDA;
-  for (int n = 0; n <= kMaxClusterParts; ++n) clusters[n] = info.clusters[n];
+  for (int n = 0; n <= kMaxClusterParts; ++n) clusters[n] = info.clusters[0][n];
   return UNSTEP_OK;
 }
 

@@ -58,6 +58,8 @@ struct AttnParams {
   int32_t run_rows[kMaxStreamsPerLaunch][3];
   int32_t run_tile_end[kMaxStreamsPerLaunch][3];
   int64_t step_base[kMaxStreamsPerLaunch];    // remainder steps of all streams before b
+  const uint32_t *scale_k, *scale_v;          // 8-bit cache: the four scale bytes of a (cache row, head) as one word
+  int64_t cache_rows;                         // 8-bit cache: rows of a stream's cache, (S + C) * T
 };
 
 // One unit of work of a worker: key tiles [t0, t1) of item (b, h, query-tile pair qp).
@@ -316,17 +318,23 @@ inline int plan_launch(AttnParams& p, const unstep_shape_t* shape, const int32_t
     p.n_sink[i] = n_sink;
     for (int r = 0; r < 3; ++r) p.run_row0[i][r] = p.run_rows[i][r] = p.run_tile_end[i][r] = 0;
     if (p.flat) {
-      // walk the attended frames in order and cut them into runs of consecutive cache slots
-      int n_runs = 0, prev_slot = -2;
-      for (int k = 0; k < n_sink + hi - lo; ++k) {
-        const int frame = k < n_sink ? k : lo + k - n_sink;
-        const int slot = frame < sink_frames ? frame : sink_frames + (frame - sink_frames) % shape->ring_frames;
-        if (slot != prev_slot + 1) {
-          if (n_runs == 3) return UNSTEP_ERR_INVALID_ARG;  // cannot happen: sink, ring end, ring start
-          p.run_row0[i][n_runs++] = slot * p.T;
-        }
-        p.run_rows[i][n_runs - 1] += p.T;
-        prev_slot = slot;
+      // the attended frames in order, as runs of consecutive cache slots: what of them lies in the sink, and in the
+      // ring up to its end and from its start
+      int n_runs = 0, end_slot = -1;
+      const auto run = [&](int slot, int frames) {
+        if (frames <= 0) return;
+        if (slot != end_slot) p.run_row0[i][n_runs++] = slot * p.T;   // else it goes on where the last one ended
+        p.run_rows[i][n_runs - 1] += frames * p.T;
+        end_slot = slot + frames;
+      };
+      run(0, n_sink);
+      const int ring_lo = lo > sink_frames ? lo : sink_frames;        // first frame that is in the ring
+      run(lo, (hi < sink_frames ? hi : sink_frames) - lo);
+      if (ring_lo < hi) {
+        const int at = (ring_lo - sink_frames) % shape->ring_frames;
+        const int to_end = shape->ring_frames - at < hi - ring_lo ? shape->ring_frames - at : hi - ring_lo;
+        run(sink_frames + at, to_end);
+        run(sink_frames, hi - ring_lo - to_end);
       }
       int tiles = 0;
       for (int r = 0; r < 3; ++r) {
@@ -392,12 +400,14 @@ inline void plan_shape(AttnParams& p, const unstep_shape_t* shape, int32_t sink_
   p.counters = nullptr;
   p.status = nullptr;
   p.extent_out = p.extent_part = p.extent_counters = 0;
+  p.scale_k = p.scale_v = nullptr;
+  p.cache_rows = 0;
 }
 
 // Argument checks shared by the attention entry points and the plan entry point (no device needed).
 inline int check_attn_args(const unstep_shape_t* shape, const int32_t* start_frame, int32_t window_frames,
-                           int32_t sink_frames, int32_t sink_attend) {
-  const int rc = check_shape(shape, true);
+                           int32_t sink_frames, int32_t sink_attend, bool partial = false) {
+  const int rc = check_shape(shape, true, partial);
   if (rc != UNSTEP_OK) return rc;
   if (start_frame == nullptr) return UNSTEP_ERR_INVALID_ARG;
   if (window_frames < shape->chunk_frames || window_frames > shape->ring_frames) return UNSTEP_ERR_INVALID_ARG;

@@ -44,14 +44,18 @@ int* status_word();
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-// Shape checks common to every call.  `need_ring` also checks batch/heads/ring_frames.
-inline int check_shape(const unstep_shape_t* s, bool need_ring) {
+// Shape checks common to every call.  `need_ring` also checks batch/heads/ring_frames.  With `partial` the
+// bands may leave a part of the head out, and an axis.
+inline int check_shape(const unstep_shape_t* s, bool need_ring, bool partial = false) {
   if (s == nullptr) return UNSTEP_ERR_INVALID_ARG;
   if (s->head_dim != kHeadDim) return s->head_dim > 0 ? UNSTEP_ERR_UNSUPPORTED : UNSTEP_ERR_INVALID_ARG;
   if (s->chunk_frames <= 0 || s->grid_h <= 0 || s->grid_w <= 0) return UNSTEP_ERR_INVALID_ARG;
-  if (s->band_t <= 0 || s->band_h <= 0 || s->band_w <= 0) return UNSTEP_ERR_INVALID_ARG;
-  if ((s->band_t | s->band_h | s->band_w) & 1) return UNSTEP_ERR_INVALID_ARG;
-  if (s->band_t + s->band_h + s->band_w != s->head_dim) return UNSTEP_ERR_INVALID_ARG;
+  const int32_t least = partial ? 0 : 1;
+  for (const int32_t d : {s->band_t, s->band_h, s->band_w})
+    if (d < least || d > s->head_dim || (d & 1)) return UNSTEP_ERR_INVALID_ARG;
+  const int32_t rotated = s->band_t + s->band_h + s->band_w;
+  if (partial ? rotated < 16 || rotated > s->head_dim || (rotated & 15) : rotated != s->head_dim)
+    return UNSTEP_ERR_INVALID_ARG;
   if (!(s->rope_base > 0.0)) return UNSTEP_ERR_INVALID_ARG;
   const int64_t T = static_cast<int64_t>(s->grid_h) * s->grid_w;
   const int64_t L = T * s->chunk_frames;
@@ -64,6 +68,19 @@ inline int check_shape(const unstep_shape_t* s, bool need_ring) {
     const int64_t ring_elems = static_cast<int64_t>(s->ring_frames) * T * s->heads * kHeadDim;
     if (ring_elems > (int64_t(1) << 38)) return UNSTEP_ERR_INVALID_ARG;
   }
+  return UNSTEP_OK;
+}
+
+// Checks of a model's kind of rotary positions, with the shape whose bands it goes with.
+inline int check_rope(const unstep_rope_t* r) {
+  if (r == nullptr || r->half < 0 || r->half > 1) return UNSTEP_ERR_INVALID_ARG;
+  bool ramp = false;
+  for (int a = 0; a < 3; ++a) {
+    if (r->trained[a] < 0 || !(r->factor[a] >= 1.0 && r->factor[a] <= 1e6)) return UNSTEP_ERR_INVALID_ARG;
+    ramp = ramp || (r->trained[a] > 0 && r->factor[a] > 1.0);
+  }
+  if (ramp && !(r->beta_slow >= 0.0 && r->beta_fast > r->beta_slow && r->beta_fast <= 1e6)) return UNSTEP_ERR_INVALID_ARG;
+  if (!(r->magnitude > 0.0 && r->magnitude <= 1e6)) return UNSTEP_ERR_INVALID_ARG;
   return UNSTEP_OK;
 }
 

@@ -13,17 +13,18 @@ namespace unstep {
 // --------------------------------------------------------------------------
 struct TableParams {
   int32_t start_frame, grid_h, grid_w, col_tiles;
-  int32_t pairs_t, pairs_h;  // pairs_w = 64 - pairs_t - pairs_h
+  int32_t pairs_t, pairs_h, pairs;   // of the time axis, of the row axis, of all three (a multiple of 8, at most kPairs)
   int* status;       // status word and extent (16-byte vectors) of each output, for checking builds
   int64_t extent;
-  double omega[kPairs];  // base^(-2i/d_band) of the 64 pairs
+  double magnitude;      // of cos and sin
+  double omega[kPairs];  // frequencies of the pairs
 };
 
-// cos and sin of position * omega in double, rounded once.
-__device__ __forceinline__ float2 table_entry(double omega, int pos) {
+// magnitude times cos and sin of position * omega in double, rounded once.
+__device__ __forceinline__ float2 table_entry(double omega, int pos, double magnitude) {
   double sn, cs;
   sincos(static_cast<double>(pos) * omega, &sn, &cs);
-  return make_float2(static_cast<float>(cs), static_cast<float>(sn));
+  return make_float2(static_cast<float>(magnitude * cs), static_cast<float>(magnitude * sn));
 }
 
 // One block per frame and tile of kTableRows x kTableCols tokens.  The table is separable: of a
@@ -41,7 +42,7 @@ rope_table_kernel(const __grid_constant__ TableParams p, float4* __restrict__ co
   const int row_tile = blockIdx.x / p.col_tiles, f = blockIdx.y;
   const int r0 = row_tile * kTableRows, c0 = (blockIdx.x - row_tile * p.col_tiles) * kTableCols;
   const int rows = min(kTableRows, p.grid_h - r0), cols = min(kTableCols, p.grid_w - c0);
-  const int n_fixed = p.pairs_t + p.pairs_h, pairs_w = kPairs - n_fixed;
+  const int n_fixed = p.pairs_t + p.pairs_h, pairs_w = p.pairs - n_fixed, quads = p.pairs / 4;
   const int row_part = p.pairs_t, col_part = row_part + rows * p.pairs_h;
   for (int e = threadIdx.x; e < col_part + cols * pairs_w; e += kTableThreads) {
     int j, pos;
@@ -57,15 +58,15 @@ rope_table_kernel(const __grid_constant__ TableParams p, float4* __restrict__ co
       j = n_fixed + (e - col_part) - c * pairs_w;
       pos = c0 + c;
     }
-    band[e] = table_entry(p.omega[j], pos);
+    band[e] = table_entry(p.omega[j], pos, p.magnitude);
   }
   __syncthreads();
   grid_launch_next();
   grid_wait();   // the evaluation above overlaps the kernel before this one, the stores do not
-  // a thread writes four pairs of a token; 16 threads write a token, so a warp stores 512 bytes of
+  // a thread writes four pairs of a token; 16 threads write a token of 64 pairs, so a warp stores 512 bytes of
   // two neighbouring tokens
-  for (int i = threadIdx.x; i < rows * cols * (kPairs / 4); i += kTableThreads) {
-    const int token = i / (kPairs / 4), quad = i % (kPairs / 4);
+  for (int i = threadIdx.x; i < rows * cols * quads; i += kTableThreads) {
+    const int token = i / quads, quad = i - token * quads;
     const int r = token / cols, c = token - r * cols;
     float2 v[4];
 #pragma unroll
@@ -76,31 +77,51 @@ rope_table_kernel(const __grid_constant__ TableParams p, float4* __restrict__ co
                                    : col_part + c * pairs_w + (j - n_fixed);
       v[u] = band[at];
     }
-    const int64_t dst = ((static_cast<int64_t>(f) * p.grid_h + r0 + r) * p.grid_w + c0 + c) * (kPairs / 4) + quad;
+    const int64_t dst = ((static_cast<int64_t>(f) * p.grid_h + r0 + r) * p.grid_w + c0 + c) * quads + quad;
     UNSTEP_STORE(cos_out, dst, p.extent, make_float4(v[0].x, v[1].x, v[2].x, v[3].x), p.status);
     UNSTEP_STORE(sin_out, dst, p.extent, make_float4(v[0].y, v[1].y, v[2].y, v[3].y), p.status);
   }
 }
 
-// Frequencies of the 64 pairs; the last set is kept per thread (64 calls of pow cost about as much
-// as the launch).
-static const double* frequency_ladder(const unstep_shape_t* s) {
+// Frequencies of the pairs of a shape, scaled as `rope` says (null: as they are); the last set is kept per thread
+// (64 calls of pow cost about as much as the launch).
+static const double* frequency_ladder(const unstep_shape_t* s, const unstep_rope_t* rope) {
   struct Ladder {
-    int32_t band_t = 0, band_h = 0, band_w = 0;
-    double base = 0.0, omega[kPairs];
+    int32_t bands[3] = {0, 0, 0}, trained[3] = {0, 0, 0};
+    double base = 0.0, factor[3] = {1.0, 1.0, 1.0}, slow = 0.0, fast = 0.0, omega[kPairs];
   };
   static thread_local Ladder l;
-  if (l.band_t != s->band_t || l.band_h != s->band_h || l.band_w != s->band_w || l.base != s->rope_base) {
-    const int32_t bands[3] = {s->band_t, s->band_h, s->band_w};
-    int j = 0;
-    for (const int32_t d : bands)
-      for (int i = 0; i < d / 2; ++i)
-        l.omega[j++] = std::pow(s->rope_base, -(2.0 * static_cast<double>(i)) / static_cast<double>(d));
-    l.band_t = s->band_t;
-    l.band_h = s->band_h;
-    l.band_w = s->band_w;
-    l.base = s->rope_base;
+  Ladder want;
+  const int32_t bands[3] = {s->band_t, s->band_h, s->band_w};
+  memcpy(want.bands, bands, sizeof(bands));
+  want.base = s->rope_base;
+  if (rope != nullptr) {
+    memcpy(want.trained, rope->trained, sizeof(want.trained));
+    memcpy(want.factor, rope->factor, sizeof(want.factor));
+    want.slow = rope->beta_slow;
+    want.fast = rope->beta_fast;
   }
+  if (memcmp(want.bands, l.bands, sizeof(l.bands)) == 0 && memcmp(want.trained, l.trained, sizeof(l.trained)) == 0 &&
+      memcmp(want.factor, l.factor, sizeof(l.factor)) == 0 && want.base == l.base && want.slow == l.slow &&
+      want.fast == l.fast)
+    return l.omega;
+  int j = 0;
+  for (int a = 0; a < 3; ++a)
+    for (int i = 0; i < bands[a] / 2; ++i) {
+      double w = std::pow(s->rope_base, -(2.0 * static_cast<double>(i)) / static_cast<double>(bands[a]));
+      if (want.factor[a] != 1.0) {
+        double keep = 0.0;
+        if (want.trained[a] > 0) {
+          const double turns = static_cast<double>(want.trained[a]) * w / 6.283185307179586476925;
+          keep = (turns - want.slow) / (want.fast - want.slow);
+          keep = keep < 0.0 ? 0.0 : (keep > 1.0 ? 1.0 : keep);
+        }
+        w *= keep + (1.0 - keep) / want.factor[a];
+      }
+      want.omega[j++] = w;
+    }
+  while (j < kPairs) want.omega[j++] = 0.0;
+  l = want;
   return l.omega;
 }
 
@@ -400,13 +421,12 @@ rmsnorm_rope_kv_append_token_kernel(AppendParams p, float eps, const uint4* q_in
 
 using namespace unstep;
 
-extern "C" int unstep_rope_table(const unstep_shape_t* shape, int32_t start_frame, float* cos_out,
-                                 float* sin_out, void* cuda_stream) {
-  int rc = check_shape(shape, false);
-  if (rc != UNSTEP_OK) return rc;
+// The table of a shape that has been checked, with its frequencies scaled as `rope` says (null: as they are).
+static int table_run(const unstep_shape_t* shape, const unstep_rope_t* rope, int32_t start_frame, float* cos_out,
+                     float* sin_out, void* cuda_stream) {
   if (start_frame < 0 || cos_out == nullptr || sin_out == nullptr) return UNSTEP_ERR_INVALID_ARG;
   if (!aligned16(cos_out) || !aligned16(sin_out)) return UNSTEP_ERR_INVALID_ARG;
-  rc = check_device();
+  const int rc = check_device();
   if (rc != UNSTEP_OK) return rc;
   if (shape->chunk_frames > 65535) return UNSTEP_ERR_INVALID_ARG;
   TableParams p;
@@ -415,9 +435,11 @@ extern "C" int unstep_rope_table(const unstep_shape_t* shape, int32_t start_fram
   p.grid_w = shape->grid_w;
   p.pairs_t = shape->band_t / 2;
   p.pairs_h = shape->band_h / 2;
+  p.pairs = (shape->band_t + shape->band_h + shape->band_w) / 2;
+  p.magnitude = rope != nullptr ? rope->magnitude : 1.0;
   p.status = status_word();
-  p.extent = static_cast<int64_t>(shape->chunk_frames) * shape->grid_h * shape->grid_w * (kPairs / 4);
-  memcpy(p.omega, frequency_ladder(shape), sizeof(p.omega));
+  p.extent = static_cast<int64_t>(shape->chunk_frames) * shape->grid_h * shape->grid_w * (p.pairs / 4);
+  memcpy(p.omega, frequency_ladder(shape, rope), sizeof(p.omega));
   p.col_tiles = (shape->grid_w + kTableCols - 1) / kTableCols;
   const dim3 grid(p.col_tiles * ((shape->grid_h + kTableRows - 1) / kTableRows), shape->chunk_frames);
   const cudaError_t err = launch_overlapped(true, rope_table_kernel, grid, kTableThreads, 0,
@@ -425,6 +447,21 @@ extern "C" int unstep_rope_table(const unstep_shape_t* shape, int32_t start_fram
                                             reinterpret_cast<float4*>(cos_out), reinterpret_cast<float4*>(sin_out));
   g_launches.fetch_add(1);
   return err == cudaSuccess ? UNSTEP_OK : UNSTEP_ERR_CUDA;
+}
+
+extern "C" int unstep_rope_table(const unstep_shape_t* shape, int32_t start_frame, float* cos_out,
+                                 float* sin_out, void* cuda_stream) {
+  const int rc = check_shape(shape, false);
+  if (rc != UNSTEP_OK) return rc;
+  return table_run(shape, nullptr, start_frame, cos_out, sin_out, cuda_stream);
+}
+
+extern "C" int unstep_rotary_table(const unstep_shape_t* shape, const unstep_rope_t* rope, int32_t start_frame,
+                                   float* cos_out, float* sin_out, void* cuda_stream) {
+  int rc = check_shape(shape, false, true);
+  if (rc == UNSTEP_OK) rc = check_rope(rope);
+  if (rc != UNSTEP_OK) return rc;
+  return table_run(shape, rope, start_frame, cos_out, sin_out, cuda_stream);
 }
 
 static int rope_kv_append_run(const unstep_shape_t* shape, int32_t sink_frames,

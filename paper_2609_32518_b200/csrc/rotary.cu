@@ -1,0 +1,537 @@
+// Rotation of one tensor by a table (HBM bound), and the append that quantises into an 8-bit cache, with the
+// read of its frames.
+#include <cuda_bf16.h>
+
+#include "common.h"
+#include "quant.cuh"
+
+namespace unstep {
+
+// What a thread rotates: 8 neighbouring dims (a 16-byte vector) at place u = 0 .. 15 of a head.
+struct RotaryPlace {
+  int32_t rows;        // float4 of a table row: R / 8
+  int32_t shift;       // halves: vectors from one half of the rotated part to the other, R / 16
+  int64_t stride4;     // table stride of a stream in float4
+  uint32_t flip;       // sign bit: the transpose
+};
+
+// Coefficients of a thread's vector.  Interleaved: of its four pairs, in the first halves of c and s.  Halves: of the 8
+// pairs that its dims belong to, s with the sign with which the partner's value comes in; y = x * c + partner * s
+// then rounds as x * c - partner * |s| does.
+template <bool kHalf>
+struct Coefficients {
+  float c[kHalf ? 8 : 4], s[kHalf ? 8 : 4];
+};
+template <bool kHalf>
+__device__ __forceinline__ Coefficients<kHalf> load_coefficients(const RotaryPlace& p, const float4* cos_t, const float4* sin_t,
+                                                                 int64_t row, int u) {
+  Coefficients<kHalf> k;
+  constexpr int kQuads = kHalf ? 2 : 1;
+  const bool second = kHalf && u >= p.shift;
+  const int64_t at = row + (kHalf ? 2 * (second ? u - p.shift : u) : u);
+#pragma unroll
+  for (int i = 0; i < kQuads; ++i) {
+    const float4 c = __ldca(cos_t + at + i), s = __ldca(sin_t + at + i);
+    k.c[4 * i] = c.x, k.c[4 * i + 1] = c.y, k.c[4 * i + 2] = c.z, k.c[4 * i + 3] = c.w;
+    k.s[4 * i] = s.x, k.s[4 * i + 1] = s.y, k.s[4 * i + 2] = s.z, k.s[4 * i + 3] = s.w;
+  }
+  const uint32_t flip = p.flip ^ (kHalf && !second ? 0x80000000u : 0u);
+#pragma unroll
+  for (int i = 0; i < 4 * kQuads; ++i) k.s[i] = __uint_as_float(__float_as_uint(k.s[i]) ^ flip);
+  return k;
+}
+
+__device__ __forceinline__ void unpack8(uint4 x, float* f) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f[2 * i] = __uint_as_float(w[i] << 16);
+    f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+  }
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  const __nv_bfloat162 y = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&y);
+}
+__device__ __forceinline__ uint4 pack8(const float* f) {
+  return make_uint4(pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7]));
+}
+
+// y = rotation of x, products and sums rounded to float32 one by one.  Halves: all lanes of the warp come here, and
+// `from` is the lane with the other half of the pairs; its values are passed as the bf16 pairs that they still are.
+__device__ __forceinline__ void rotate_pairs(const float* x, const Coefficients<false>& k, float* y) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    y[2 * i] = __fsub_rn(__fmul_rn(x[2 * i], k.c[i]), __fmul_rn(x[2 * i + 1], k.s[i]));
+    y[2 * i + 1] = __fadd_rn(__fmul_rn(x[2 * i], k.s[i]), __fmul_rn(x[2 * i + 1], k.c[i]));
+  }
+}
+__device__ __forceinline__ void rotate_halves(const float* x, const float* other, const Coefficients<true>& k, float* y) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) y[i] = __fadd_rn(__fmul_rn(x[i], k.c[i]), __fmul_rn(other[i], k.s[i]));
+}
+__device__ __forceinline__ uint4 shuffle16(uint4 x, int from) {
+  return make_uint4(__shfl_sync(0xFFFFFFFFu, x.x, from), __shfl_sync(0xFFFFFFFFu, x.y, from),
+                    __shfl_sync(0xFFFFFFFFu, x.z, from), __shfl_sync(0xFFFFFFFFu, x.w, from));
+}
+__device__ __forceinline__ int partner_lane(const RotaryPlace& p, int lane, int u, bool rotated) {
+  return rotated ? (u >= p.shift ? lane - p.shift : lane + p.shift) : lane;
+}
+
+// --------------------------------------------------------------------------
+// Rotation of one tensor.  A thread has the same place of up to kApplyHeads heads of a token: it fetches
+// its coefficients once, and its loads are in flight together.
+// --------------------------------------------------------------------------
+constexpr int kApplyHeads = 4;
+
+struct ApplyParams {
+  RotaryPlace place;
+  int64_t vec_per_stream;      // L * Hn * 16
+  int64_t threads_per_stream;  // L * width
+  int32_t width;               // threads of a token: 16 * ceil(Hn / kApplyHeads)
+  int32_t vec_per_token;       // Hn * 16
+  int* status;
+  int64_t extent;
+};
+
+template <bool kHalf>
+__global__ void __launch_bounds__(256)
+rotary_apply_kernel(const ApplyParams p, const uint4* x_in, const float4* cos_t, const float4* sin_t, uint4* y_out) {
+  grid_launch_next();
+  const int64_t id = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
+  const int b = blockIdx.y;
+  const bool live = id < p.threads_per_stream;
+  const int64_t n = id / p.width;
+  const int i0 = static_cast<int>(id - n * p.width), u = i0 & 15;
+  const bool rotated = u < p.place.rows;
+  const int behind = grid_wait();
+  const int64_t base = static_cast<int64_t>(b) * p.vec_per_stream + n * p.vec_per_token + behind;
+  uint4 x[kApplyHeads];
+#pragma unroll
+  for (int j = 0; j < kApplyHeads; ++j) {
+    const int i = i0 + j * p.width;
+    x[j] = make_uint4(0, 0, 0, 0);
+    if (live && i < p.vec_per_token) x[j] = __ldcs(x_in + base + i);
+  }
+  Coefficients<kHalf> k = {};
+  if (live && rotated) k = load_coefficients<kHalf>(p.place, cos_t, sin_t, b * p.place.stride4 + n * p.place.rows + behind, u);
+  const int from = partner_lane(p.place, threadIdx.x & 31, u, rotated);
+#pragma unroll
+  for (int j = 0; j < kApplyHeads; ++j) {
+    const int i = i0 + j * p.width;
+    float f[8], y[8];
+    unpack8(x[j], f);
+    if constexpr (kHalf) {
+      float other[8];
+      unpack8(shuffle16(x[j], from), other);
+      rotate_halves(f, other, k, y);
+    } else {
+      rotate_pairs(f, k, y);
+    }
+    if (live && i < p.vec_per_token) UNSTEP_STORE(y_out, base + i, p.extent, rotated ? pack8(y) : x[j], p.status);
+  }
+}
+
+// --------------------------------------------------------------------------
+// Append into the 8-bit cache.  A thread has the same place of kU heads of a token in q, k and v, `width` vectors
+// apart; without the norm the threads of all tokens are one sequence, with it a block has a token (kWide: more
+// vectors than its threads hold, read a second time behind the sum of squares).  Four neighbouring threads
+// hold a block of 32 dims and find its largest magnitude with two shuffles.
+// --------------------------------------------------------------------------
+struct Append8Params {
+  RotaryPlace place;
+  int32_t L, T, C, S, vec_per_token, width;
+  int64_t vec_per_stream;          // L * Hn * 16
+  int64_t cache_vec_per_stream;    // (S + C) * T * Hn * 16 vectors of 8 codes
+  float eps;
+  int32_t start[kMaxStreamsPerLaunch];
+  int* status;                     // extents of q_out (16-byte vectors), codes (8-byte vectors) and scale bytes
+  int64_t extent_act, extent_code, extent_scale;
+};
+
+__device__ __forceinline__ float warp_sum32(float x) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
+  return x;
+}
+__device__ __forceinline__ float squares32(uint4 x, float acc) {
+  float f[8];
+  unpack8(x, f);
+  float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    s0 = fmaf(f[2 * i], f[2 * i], s0);
+    s1 = fmaf(f[2 * i + 1], f[2 * i + 1], s1);
+  }
+  return acc + (s0 + s1);
+}
+__device__ __forceinline__ void gain8(float* f, float r, const float4* gain, int vi) {
+  const float4 g0 = __ldca(gain + 2 * vi), g1 = __ldca(gain + 2 * vi + 1);
+  const float g[8] = {g0.x, g0.y, g0.z, g0.w, g1.x, g1.y, g1.z, g1.w};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] = __fmul_rn(__fmul_rn(f[i], r), g[i]);
+}
+
+template <int kU, bool kHalf, bool kNorm, bool kWide>
+__global__ void __launch_bounds__(256)
+rotary_kv_append_q8_kernel(const Append8Params p, const uint4* q_in, const uint4* k_in, const uint4* v_in,
+                           const float4* gain_q, const float4* gain_k, const float4* cos_t, const float4* sin_t,
+                           uint4* q_out, uint2* cache_k, uint8_t* scale_k, uint2* cache_v, uint8_t* scale_v) {
+  __shared__ float part[2][8];
+  grid_launch_next();
+  const int b = blockIdx.y;
+  int n, i0;
+  if (kNorm) {
+    n = blockIdx.x;
+    i0 = threadIdx.x;
+  } else {
+    const int64_t id = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
+    n = static_cast<int>(id / p.width);
+    i0 = static_cast<int>(id - static_cast<int64_t>(n) * p.width);
+  }
+  const bool live = n < p.L;
+  const int f = n / p.T, t = n - f * p.T;
+  const int frame = p.start[b] + f;
+  const int slot = frame < p.S ? frame : p.S + (frame - p.S) % p.C;
+  const int u = i0 & 15;
+  const bool rotated = u < p.place.rows;
+  const int behind = grid_wait();
+  i0 += behind;   // every load below goes by i0
+  const int64_t in_base = static_cast<int64_t>(b) * p.vec_per_stream + static_cast<int64_t>(n) * p.vec_per_token;
+  const int64_t cache_base = static_cast<int64_t>(b) * p.cache_vec_per_stream +
+                             (static_cast<int64_t>(slot) * p.T + t) * p.vec_per_token;
+  const int from = partner_lane(p.place, threadIdx.x & 31, u, rotated);
+  const int step = p.width * kU;
+  const uint4 zero = make_uint4(0, 0, 0, 0);
+
+  uint4 xq[kU], xk[kU], xv[kU];
+  auto load = [&](int at) {
+#pragma unroll
+    for (int j = 0; j < kU; ++j) {
+      const int i = at + j * p.width;
+      const bool mine = live && i < p.vec_per_token;
+      xq[j] = mine ? q_in[in_base + i] : zero;   // plain load: q_out may be the same buffer
+      xk[j] = mine ? __ldca(k_in + in_base + i) : zero;
+      xv[j] = mine ? __ldcs(v_in + in_base + i) : zero;
+    }
+  };
+  float rq = 1.f, rk = 1.f;
+  load(i0);
+  Coefficients<kHalf> k = {};
+  if (live && rotated)
+    k = load_coefficients<kHalf>(p.place, cos_t, sin_t, b * p.place.stride4 + static_cast<int64_t>(n) * p.place.rows + behind, u);
+  if (kNorm) {
+    float sq = 0.f, sk = 0.f;
+    for (int at = i0;;) {
+#pragma unroll
+      for (int j = 0; j < kU; ++j) {
+        sq = squares32(xq[j], sq);
+        sk = squares32(xk[j], sk);
+      }
+      at += step;
+      if (!kWide || at - i0 >= p.vec_per_token) break;
+      load(at);
+    }
+    sq = warp_sum32(sq);
+    sk = warp_sum32(sk);
+    if ((threadIdx.x & 31) == 0) {
+      part[0][threadIdx.x >> 5] = sq;
+      part[1][threadIdx.x >> 5] = sk;
+    }
+    __syncthreads();
+    sq = sk = 0.f;
+    for (int w = 0; w < static_cast<int>(blockDim.x >> 5); ++w) {
+      sq += part[0][w];
+      sk += part[1][w];
+    }
+    const float width = static_cast<float>(p.vec_per_token) * 8.f;
+    rq = __frcp_rn(__fsqrt_rn(__fadd_rn(__fdiv_rn(sq, width), p.eps)));
+    rk = __frcp_rn(__fsqrt_rn(__fadd_rn(__fdiv_rn(sk, width), p.eps)));
+    if (kWide) load(i0);
+  }
+  // float32 values behind the norm and the rotation
+  auto turn = [&](uint4 x, float r, const float4* gain, int vi, float* y) {
+    float v[8];
+    unpack8(x, v);
+    if (kNorm && vi < p.vec_per_token) gain8(v, r, gain, vi);
+    if constexpr (kHalf) {
+      float other[8];
+      if (kNorm) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) other[e] = __shfl_sync(0xFFFFFFFFu, v[e], from);
+      } else {
+        unpack8(shuffle16(x, from), other);
+      }
+      rotate_halves(v, other, k, y);
+    } else {
+      rotate_pairs(v, k, y);
+    }
+    if (!rotated) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = v[e];
+    }
+  };
+  for (int at = i0;;) {
+#pragma unroll
+    for (int j = 0; j < kU; ++j) {
+      const int i = at + j * p.width;
+      const bool mine = live && i < p.vec_per_token;
+      float y[8];
+      turn(xq[j], rq, gain_q, i, y);
+      if (mine) UNSTEP_STORE(q_out, in_base + i, p.extent_act, pack8(y), p.status);
+      uint32_t byte_k, byte_v;
+      turn(xk[j], rk, gain_k, i, y);
+      const uint2 ck = q8::quantise8(y, &byte_k);
+      unpack8(xv[j], y);
+      const uint2 cv = q8::quantise8(y, &byte_v);
+      if (mine) {
+        const int64_t dst = cache_base + i;
+        UNSTEP_STORE(cache_k, dst, p.extent_code, ck, p.status);
+        UNSTEP_STORE(cache_v, dst, p.extent_code, cv, p.status);
+        if ((u & 3) == 0) {
+          UNSTEP_STORE(scale_k, dst >> 2, p.extent_scale, static_cast<uint8_t>(byte_k), p.status);
+          UNSTEP_STORE(scale_v, dst >> 2, p.extent_scale, static_cast<uint8_t>(byte_v), p.status);
+        }
+      }
+    }
+    at += step;
+    if (!kWide || at - i0 >= p.vec_per_token) break;
+    load(at);
+  }
+}
+
+// --------------------------------------------------------------------------
+// Frames of the 8-bit cache as bf16.  A thread decodes 16 codes of k and of v; a block stays in one frame.
+// --------------------------------------------------------------------------
+struct Read8Params {
+  int32_t C, S, n_frames, frame0;      // frame0: first frame of this launch inside the read
+  int64_t vec_per_frame;               // T * Hn * 8 vectors of 16 codes
+  int64_t cache_vec_per_stream;
+  int32_t first[kMaxStreamsPerLaunch];
+  int* status;
+  int64_t extent;                      // 16-byte vectors of an output
+};
+
+__device__ __forceinline__ void store_decoded(uint4* out, int64_t dst, int64_t extent, uint4 x, uint32_t byte, int* status) {
+  const uint32_t f1 = q8::factor1(byte);
+  uint4 lo = q8::decode8(x.x, x.y, f1), hi = q8::decode8(x.z, x.w, f1);
+  if (!q8::one_factor(byte)) {
+    const uint32_t f2 = q8::factor2(byte);
+    lo = q8::mul8(lo, f2);
+    hi = q8::mul8(hi, f2);
+  }
+  UNSTEP_STORE(out, dst, extent, lo, status);
+  UNSTEP_STORE(out, dst + 1, extent, hi, status);
+}
+
+__global__ void __launch_bounds__(256)
+kv_read_q8_kernel(const Read8Params p, const uint4* cache_k, const uint8_t* scale_k, const uint4* cache_v,
+                  const uint8_t* scale_v, uint4* out_k, uint4* out_v) {
+  grid_launch_next();
+  const int64_t v = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
+  const int behind = grid_wait();
+  if (v >= p.vec_per_frame) return;
+  const int b = blockIdx.z, f = p.frame0 + blockIdx.y;
+  const int frame = p.first[b] + f;
+  const int slot = frame < p.S ? frame : p.S + (frame - p.S) % p.C;
+  const int64_t src = b * p.cache_vec_per_stream + slot * p.vec_per_frame + v + behind;
+  const uint4 xk = __ldcs(cache_k + src), xv = __ldcs(cache_v + src);
+  const uint32_t ek = __ldca(scale_k + (src >> 1)), ev = __ldca(scale_v + (src >> 1));
+  const int64_t dst = 2 * ((static_cast<int64_t>(b) * p.n_frames + f) * p.vec_per_frame + v);
+  store_decoded(out_k, dst, p.extent, xk, ek, p.status);
+  store_decoded(out_v, dst, p.extent, xv, ev, p.status);
+}
+
+static RotaryPlace rotary_place(const unstep_shape_t* s, int64_t table_stream_stride, bool transposed) {
+  const int32_t rotated = s->band_t + s->band_h + s->band_w;
+  RotaryPlace p;
+  p.rows = rotated / 8;
+  p.shift = rotated / 16;
+  p.stride4 = table_stream_stride / 4;
+  p.flip = transposed ? 0x80000000u : 0u;
+  return p;
+}
+
+static bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+}  // namespace unstep
+
+using namespace unstep;
+
+extern "C" int unstep_rotary_apply(const unstep_shape_t* shape, const unstep_rope_t* rope, int32_t transposed,
+                                   const void* x, const float* cos, const float* sin, int64_t table_stream_stride,
+                                   void* y, void* cuda_stream) {
+  int rc = check_shape(shape, false, true);
+  if (rc == UNSTEP_OK) rc = check_rope(rope);
+  if (rc != UNSTEP_OK) return rc;
+  if (shape->batch <= 0 || shape->batch > (1 << 20) || shape->heads <= 0 || shape->heads > 4096) return UNSTEP_ERR_INVALID_ARG;
+  if (transposed < 0 || transposed > 1) return UNSTEP_ERR_INVALID_ARG;
+  const void* ptrs[] = {x, cos, sin, y};
+  for (const void* ptr : ptrs)
+    if (ptr == nullptr || !aligned16(ptr)) return UNSTEP_ERR_INVALID_ARG;
+  if (table_stream_stride < 0 || (table_stream_stride & 3)) return UNSTEP_ERR_INVALID_ARG;
+  rc = check_device();
+  if (rc != UNSTEP_OK) return rc;
+  const int64_t L = static_cast<int64_t>(shape->grid_h) * shape->grid_w * shape->chunk_frames;
+  ApplyParams p;
+  p.place = rotary_place(shape, table_stream_stride, transposed != 0);
+  p.vec_per_token = shape->heads * 16;
+  p.width = 16 * ((shape->heads + kApplyHeads - 1) / kApplyHeads);
+  p.vec_per_stream = L * p.vec_per_token;
+  p.threads_per_stream = L * p.width;
+  const int64_t blocks = (p.threads_per_stream + 255) / 256;
+  if (blocks > INT32_MAX) return UNSTEP_ERR_INVALID_ARG;
+  p.status = status_word();
+  constexpr int kMaxStreams = 65535;
+  for (int b0 = 0; b0 < shape->batch; b0 += kMaxStreams) {
+    const int nb = shape->batch - b0 < kMaxStreams ? shape->batch - b0 : kMaxStreams;
+    p.extent = nb * p.vec_per_stream;
+    const int64_t off = b0 * p.vec_per_stream, tab = b0 * table_stream_stride;
+    const cudaError_t err = launch_overlapped(
+        true, rope->half ? rotary_apply_kernel<true> : rotary_apply_kernel<false>, dim3(static_cast<unsigned>(blocks), nb), 256,
+        0, static_cast<cudaStream_t>(cuda_stream), p, static_cast<const uint4*>(x) + off,
+        reinterpret_cast<const float4*>(cos + tab), reinterpret_cast<const float4*>(sin + tab), static_cast<uint4*>(y) + off);
+    g_launches.fetch_add(1);
+    if (err != cudaSuccess) return UNSTEP_ERR_CUDA;
+  }
+  return UNSTEP_OK;
+}
+
+namespace unstep {
+typedef void (*Append8Kernel)(const Append8Params, const uint4*, const uint4*, const uint4*, const float4*, const float4*,
+                              const float4*, const float4*, uint4*, uint2*, uint8_t*, uint2*, uint8_t*);
+template <bool kHalf>
+static Append8Kernel append8_kernel(bool norm, int per_thread, bool wide) {
+  if (!norm) return per_thread == 1 ? rotary_kv_append_q8_kernel<1, kHalf, false, false> : rotary_kv_append_q8_kernel<2, kHalf, false, false>;
+  if (wide) return rotary_kv_append_q8_kernel<4, kHalf, true, true>;
+  switch (per_thread) {
+    case 1: return rotary_kv_append_q8_kernel<1, kHalf, true, false>;
+    case 2: return rotary_kv_append_q8_kernel<2, kHalf, true, false>;
+    case 3: return rotary_kv_append_q8_kernel<3, kHalf, true, false>;
+    default: return rotary_kv_append_q8_kernel<4, kHalf, true, false>;
+  }
+}
+}  // namespace unstep
+
+extern "C" int unstep_rotary_kv_append_q8(const unstep_shape_t* shape, const unstep_rope_t* rope, int32_t sink_frames,
+                                          const int32_t* start_frame, const void* q_in, const void* k_in,
+                                          const void* v_in, const float* gain_q, const float* gain_k, float eps,
+                                          const float* cos, const float* sin, int64_t table_stream_stride, void* q_out,
+                                          void* cache_k, void* scale_k, void* cache_v, void* scale_v, void* cuda_stream) {
+  int rc = check_shape(shape, true, true);
+  if (rc == UNSTEP_OK) rc = check_rope(rope);
+  if (rc != UNSTEP_OK) return rc;
+  const bool norm = gain_q != nullptr;
+  if (sink_frames < 0 || sink_frames > 4096 || norm != (gain_k != nullptr) || (norm && !(eps >= 0.f)))
+    return UNSTEP_ERR_INVALID_ARG;
+  const void* ptrs[] = {q_in, k_in, v_in, cos, sin, q_out, cache_k, cache_v};
+  for (const void* ptr : ptrs)
+    if (ptr == nullptr || !aligned16(ptr)) return UNSTEP_ERR_INVALID_ARG;
+  if (start_frame == nullptr || scale_k == nullptr || scale_v == nullptr || !aligned4(scale_k) || !aligned4(scale_v) ||
+      !aligned16(gain_q) || !aligned16(gain_k))
+    return UNSTEP_ERR_INVALID_ARG;
+  if (table_stream_stride < 0 || (table_stream_stride & 3)) return UNSTEP_ERR_INVALID_ARG;
+  for (int b = 0; b < shape->batch; ++b)
+    if (start_frame[b] < 0 || start_frame[b] > INT32_MAX - shape->chunk_frames) return UNSTEP_ERR_INVALID_ARG;
+  rc = check_device();
+  if (rc != UNSTEP_OK) return rc;
+
+  const int64_t T = static_cast<int64_t>(shape->grid_h) * shape->grid_w;
+  const int64_t L = T * shape->chunk_frames;
+  Append8Params p;
+  p.place = rotary_place(shape, table_stream_stride, false);
+  p.L = static_cast<int32_t>(L);
+  p.T = static_cast<int32_t>(T);
+  p.C = shape->ring_frames;
+  p.S = sink_frames;
+  p.vec_per_token = shape->heads * 16;
+  p.vec_per_stream = L * p.vec_per_token;
+  p.cache_vec_per_stream = (static_cast<int64_t>(shape->ring_frames) + sink_frames) * T * p.vec_per_token;
+  p.eps = eps;
+  p.status = status_word();
+  int threads = 256, per_thread = 1;
+  bool wide = false;
+  int64_t blocks;
+  if (norm) {
+    per_thread = (p.vec_per_token + 95) / 96;
+    if (per_thread > 4) per_thread = 4;
+    threads = (((p.vec_per_token + per_thread - 1) / per_thread) + 31) & ~31;
+    wide = threads > 256;
+    if (wide) threads = 256;
+    p.width = threads;
+    blocks = L;
+  } else {
+    per_thread = shape->heads > 1 ? 2 : 1;
+    p.width = 16 * ((shape->heads + per_thread - 1) / per_thread);
+    blocks = (L * p.width + 255) / 256;
+  }
+  if (blocks > INT32_MAX) return UNSTEP_ERR_INVALID_ARG;
+  const Append8Kernel kernel = rope->half ? append8_kernel<true>(norm, per_thread, wide) : append8_kernel<false>(norm, per_thread, wide);
+  for (int b0 = 0; b0 < shape->batch; b0 += kMaxStreamsPerLaunch) {
+    const int nb = shape->batch - b0 < kMaxStreamsPerLaunch ? shape->batch - b0 : kMaxStreamsPerLaunch;
+    for (int i = 0; i < nb; ++i) p.start[i] = start_frame[b0 + i];
+    p.extent_act = nb * p.vec_per_stream;
+    p.extent_code = nb * p.cache_vec_per_stream;
+    p.extent_scale = p.extent_code / 4;
+    const int64_t in = b0 * p.vec_per_stream, cache = b0 * p.cache_vec_per_stream, tab = b0 * table_stream_stride;
+    const cudaError_t err = launch_overlapped(
+        true, kernel, dim3(static_cast<unsigned>(blocks), nb), threads, 0, static_cast<cudaStream_t>(cuda_stream), p,
+        static_cast<const uint4*>(q_in) + in, static_cast<const uint4*>(k_in) + in, static_cast<const uint4*>(v_in) + in,
+        reinterpret_cast<const float4*>(gain_q), reinterpret_cast<const float4*>(gain_k),
+        reinterpret_cast<const float4*>(cos + tab), reinterpret_cast<const float4*>(sin + tab), static_cast<uint4*>(q_out) + in,
+        static_cast<uint2*>(cache_k) + cache, static_cast<uint8_t*>(scale_k) + cache / 4, static_cast<uint2*>(cache_v) + cache,
+        static_cast<uint8_t*>(scale_v) + cache / 4);
+    g_launches.fetch_add(1);
+    if (err != cudaSuccess) return UNSTEP_ERR_CUDA;
+  }
+  return UNSTEP_OK;
+}
+
+extern "C" int unstep_kv_read_q8(const unstep_shape_t* shape, int32_t sink_frames, const int32_t* first_frame,
+                                 int32_t n_frames, const void* cache_k, const void* scale_k, const void* cache_v,
+                                 const void* scale_v, void* out_k, void* out_v, void* cuda_stream) {
+  int rc = check_shape(shape, true, true);
+  if (rc != UNSTEP_OK) return rc;
+  if (sink_frames < 0 || sink_frames > 4096 || n_frames < 1 || first_frame == nullptr) return UNSTEP_ERR_INVALID_ARG;
+  const void* ptrs[] = {cache_k, cache_v, out_k, out_v};
+  for (const void* ptr : ptrs)
+    if (ptr == nullptr || !aligned16(ptr)) return UNSTEP_ERR_INVALID_ARG;
+  if (scale_k == nullptr || scale_v == nullptr || !aligned4(scale_k) || !aligned4(scale_v)) return UNSTEP_ERR_INVALID_ARG;
+  for (int b = 0; b < shape->batch; ++b) {
+    if (first_frame[b] < 0 || first_frame[b] > INT32_MAX - n_frames) return UNSTEP_ERR_INVALID_ARG;
+    const int32_t ring0 = first_frame[b] > sink_frames ? first_frame[b] : sink_frames;   // first one behind the sink
+    if (first_frame[b] + n_frames - ring0 > shape->ring_frames) return UNSTEP_ERR_INVALID_ARG;
+  }
+  rc = check_device();
+  if (rc != UNSTEP_OK) return rc;
+  const int64_t T = static_cast<int64_t>(shape->grid_h) * shape->grid_w;
+  Read8Params p;
+  p.C = shape->ring_frames;
+  p.S = sink_frames;
+  p.n_frames = n_frames;
+  p.vec_per_frame = T * shape->heads * 8;
+  p.cache_vec_per_stream = (static_cast<int64_t>(shape->ring_frames) + sink_frames) * p.vec_per_frame;
+  p.status = status_word();
+  const int64_t blocks = (p.vec_per_frame + 255) / 256;
+  if (blocks > INT32_MAX) return UNSTEP_ERR_INVALID_ARG;
+  constexpr int kMaxFrames = 65535;
+  for (int b0 = 0; b0 < shape->batch; b0 += kMaxStreamsPerLaunch) {
+    const int nb = shape->batch - b0 < kMaxStreamsPerLaunch ? shape->batch - b0 : kMaxStreamsPerLaunch;
+    for (int i = 0; i < nb; ++i) p.first[i] = first_frame[b0 + i];
+    const int64_t cache = b0 * p.cache_vec_per_stream;
+    const int64_t out = 2 * static_cast<int64_t>(b0) * n_frames * p.vec_per_frame;
+    p.extent = 2 * static_cast<int64_t>(nb) * n_frames * p.vec_per_frame;
+    for (p.frame0 = 0; p.frame0 < n_frames; p.frame0 += kMaxFrames) {
+      const int nf = n_frames - p.frame0 < kMaxFrames ? n_frames - p.frame0 : kMaxFrames;
+      const cudaError_t err = launch_overlapped(
+          true, kv_read_q8_kernel, dim3(static_cast<unsigned>(blocks), nf, nb), 256, 0, static_cast<cudaStream_t>(cuda_stream),
+          p, static_cast<const uint4*>(cache_k) + cache, static_cast<const uint8_t*>(scale_k) + cache / 2,
+          static_cast<const uint4*>(cache_v) + cache, static_cast<const uint8_t*>(scale_v) + cache / 2,
+          static_cast<uint4*>(out_k) + out, static_cast<uint4*>(out_v) + out);
+      g_launches.fetch_add(1);
+      if (err != cudaSuccess) return UNSTEP_ERR_CUDA;
+      if (n_frames - p.frame0 <= kMaxFrames) break;
+    }
+  }
+  return UNSTEP_OK;
+}
