@@ -968,6 +968,66 @@ __global__ void wait_limit_probe_kernel(long long limit_cycles) {
 }
 
 // --------------------------------------------------------------------------
+// Keys and values of an 8-bit cache's windows as bf16, for launches that read them often: per stream and head the
+// keys of the window in order, padded with zeros to whole tiles.  A thread decodes 16 dims of k and v of kUnpackRows
+// rows, 32 apart; eight threads have a row of a head, 128 bytes in and 256 out.  DRAM bound.
+// --------------------------------------------------------------------------
+constexpr int kUnpackRows = 2;
+struct Unpack8Params {
+  int32_t Hn, head0, rows;             // heads of the cache, first head of this launch, rows that the output has for a stream
+  int64_t cache_rows;
+  int32_t run_row0[kMaxStreamsPerLaunch][3], run_end[kMaxStreamsPerLaunch][3];   // rows of the runs, added up
+  int* status;
+  int64_t extent;                      // 16-byte vectors of an output
+};
+
+__device__ __forceinline__ void store_unpacked(uint4* out, int64_t dst, int64_t extent, uint4 x, uint32_t byte, int* status) {
+  const uint32_t f1 = q8::factor1(byte);
+  uint4 y[2] = {q8::decode8(x.x, x.y, f1), q8::decode8(x.z, x.w, f1)};
+  if (!q8::one_factor(byte)) {
+    const uint32_t f2 = q8::factor2(byte);
+    y[0] = q8::mul8(y[0], f2);
+    y[1] = q8::mul8(y[1], f2);
+  }
+  UNSTEP_STORE_32(out, dst, extent, reinterpret_cast<const uint32_t*>(y), status);
+}
+
+__global__ void __launch_bounds__(256)
+window_unpack_q8_kernel(const __grid_constant__ Unpack8Params p, const uint4* cache_k, const uint8_t* scale_k, const uint4* cache_v,
+                        const uint8_t* scale_v, uint4* out_k, uint4* out_v) {
+  grid_launch_next();
+  const int b = blockIdx.z, h = blockIdx.y, vec = threadIdx.x & 7;
+  const int row0 = static_cast<int>(blockIdx.x) * 32 * kUnpackRows + (threadIdx.x >> 3);
+  const int behind = grid_wait();
+  uint4 xk[kUnpackRows], xv[kUnpackRows];
+  uint32_t ek[kUnpackRows], ev[kUnpackRows];
+#pragma unroll
+  for (int i = 0; i < kUnpackRows; ++i) {
+    const int r = row0 + 32 * i;
+    xk[i] = xv[i] = make_uint4(0, 0, 0, 0);
+    ek[i] = ev[i] = q8::kLeastByte;
+    if (r < p.run_end[b][2]) {
+      const int run = r < p.run_end[b][0] ? 0 : (r < p.run_end[b][1] ? 1 : 2);
+      const int row = p.run_row0[b][run] + r - (run == 0 ? 0 : p.run_end[b][run - 1]);
+      const int64_t src = ((b * p.cache_rows + row) * p.Hn + p.head0 + h) * 8 + vec + behind;
+      xk[i] = __ldcs(cache_k + src);
+      xv[i] = __ldcs(cache_v + src);
+      ek[i] = __ldca(scale_k + (src >> 1));
+      ev[i] = __ldca(scale_v + (src >> 1));
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kUnpackRows; ++i) {
+    const int r = row0 + 32 * i;
+    if (r < (p.run_end[b][2] + kTileN - 1) / kTileN * kTileN) {
+      const int64_t dst = 2 * (((static_cast<int64_t>(b) * gridDim.y + h) * p.rows + r) * 8 + vec);
+      store_unpacked(out_k, dst, p.extent, xk[i], ek[i], p.status);
+      store_unpacked(out_v, dst, p.extent, xv[i], ev[i], p.status);
+    }
+  }
+}
+
+// --------------------------------------------------------------------------
 // Host side
 // --------------------------------------------------------------------------
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
@@ -1081,10 +1141,16 @@ struct Workspace {
 };
 constexpr size_t kLeastCounters = 4096;
 constexpr int kMaxGrowths = 32;
+constexpr size_t kLeastWindow = size_t{16} << 20;
+constexpr int kWindowSizes = 5;                                           // up to 256 MB
+constexpr size_t kMostWindow = kLeastWindow << (kWindowSizes - 1);
 struct StreamScratch {
   Workspace ws;
   Workspace left[kMaxGrowths];   // counters of former calls; captured graphs may still count in them
   int n_left = 0;
+  // unpacked windows of an 8-bit cache: the last one is in use, the smaller ones may be in captured graphs
+  void* window[kWindowSizes] = {};
+  int n_windows = 0;             // window[i] has kLeastWindow << i bytes, or is null
 };
 static std::mutex g_ws_mutex;
 static std::map<std::pair<int, cudaStream_t>, StreamScratch> g_workspaces;
@@ -1119,6 +1185,31 @@ static int get_workspace(cudaStream_t st, size_t slots, size_t n_counters, Works
   }
   *out = ws;
   return UNSTEP_OK;
+}
+
+// `bytes` (at most kMostWindow) for unpacked windows on this stream; null if there is no room, or if the stream
+// is being captured and the buffer would have to be made.
+static void* get_window(cudaStream_t st, size_t bytes) {
+  int dev = 0;
+  if (bytes > kMostWindow || cudaGetDevice(&dev) != cudaSuccess) return nullptr;
+  int size = 0;
+  while (kLeastWindow << size < bytes) ++size;
+  std::lock_guard<std::mutex> lock(g_ws_mutex);
+  StreamScratch& s = g_workspaces[std::make_pair(dev, st)];
+  if (s.n_windows > size) return s.window[s.n_windows - 1];
+  cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+  if (cudaStreamIsCapturing(st, &capture) != cudaSuccess || capture != cudaStreamCaptureStatusNone) {
+    cudaGetLastError();
+    return nullptr;
+  }
+  void* made = nullptr;
+  if (cudaMalloc(&made, kLeastWindow << size) != cudaSuccess) {
+    cudaGetLastError();
+    return nullptr;
+  }
+  s.window[size] = made;
+  s.n_windows = size + 1;
+  return made;
 }
 
 // After a kernel gave up, arrival counters may be left non-zero: clear them all.
@@ -1159,6 +1250,46 @@ typedef int (*ScratchFn)(cudaStream_t st, size_t slots, size_t n_counters, Works
 
 constexpr int kOverlapSteps = 64;   // key-tile steps per worker below which a launch overlaps the kernel before it
 
+// Launches a planned kernel.
+//
+// Set up under the append before it where the launch is short.  Append and attention (with the pipeline of one
+// S per query tile, 10 % slower per step), us not
+// overlapped -> overlapped, by steps per worker: in runs of 20 (full clock) 24: 78.9 -> 76.5, 35:
+// 94.6 -> 92.6, 57: 143.1 -> 142.3, 114: 242.0 -> 240.6, 226: 446.1 -> 445.5, 394: 754.9 -> 763.7; run
+// on end at the power cap 24: 80.2 -> 79.8 (1912 -> 1867 MHz), 57: 155.2 -> 155.8 (1792 -> 1776), 114:
+// 276.7 -> 276.6 (1702 -> 1688), 169: 395.4 -> 398.6 (1680 -> 1652), 394: 880.4 -> 895.9 (1635 -> 1605).
+// The overlap saves 1.5-6 thousand cycles of a launch at any length; at the cap the clock falls for
+// the idling it takes away.  The line lies about where the gain of short runs (0.6 % at 57 steps) has
+// come down to the loss of runs at the cap (0.4 %).
+static int launch_attn(const AttnParams& p, bool q8, const CUtensorMap& tm_q, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
+                       const CUtensorMap& tm_kf, const CUtensorMap& tm_vf, __nv_bfloat16* out, cudaStream_t st) {
+  const bool brief = p.all_steps < static_cast<int64_t>(kOverlapSteps) * p.n_workers;
+  const cudaError_t err =
+      launch_clusters(brief, p.cluster ? p.parts : 1,
+                      q8 ? (p.cluster ? window_attn_kernel<true, true> : window_attn_kernel<false, true>)
+                         : (p.cluster ? window_attn_kernel<true, false> : window_attn_kernel<false, false>),
+                      p.n_workers, q8 ? Form<true>::kThreads : Form<false>::kThreads, kAttnSmemBytes, st, tm_q, tm_k, tm_v,
+                      tm_kf, tm_vf, p, out);
+  g_launches.fetch_add(1);
+  return err == cudaSuccess ? UNSTEP_OK : UNSTEP_ERR_CUDA;
+}
+
+// The scratch and the checking build's extents of a planned launch whose results start at `out`, `skip` 16-byte vectors
+// into the first stream's.
+static int bind_scratch(AttnParams& p, cudaStream_t st, ScratchFn scratch, int sm_count, const void* out, int64_t skip) {
+  Workspace ws;
+  const int rc = scratch(st, 2 * static_cast<size_t>(sm_count), 2 * static_cast<size_t>(p.n_streams) * p.items_per_stream, &ws);
+  if (rc != UNSTEP_OK) return rc;
+  p.part = ws.part;
+  p.counters = ws.counters;
+  p.status = status_word();
+  p.out_wide = (reinterpret_cast<uintptr_t>(out) & 31u) == 0;   // rows are multiples of 256 bytes
+  p.extent_out = static_cast<int64_t>(p.n_streams) * p.L * p.Hn * (kHeadDim / 8) - skip;
+  p.extent_part = static_cast<int64_t>(ws.slots) * kPartFloats;
+  p.extent_counters = static_cast<int64_t>(ws.n_counters);
+  return UNSTEP_OK;
+}
+
 // Validation, work split, tensor maps and launch shared by the attention entry points.
 // The cache has `sink_frames` slots in front of the ring (0 for the plain rolling window);
 // stream b attends frames [0, min(sink_attend, lo)) and [lo, hi), lo = max(0, hi - window_frames).
@@ -1195,16 +1326,8 @@ static int window_attn_run(const unstep_shape_t* shape, const int32_t* start_fra
     rc = plan_launch(p, shape, start_frame + b0, nb, window_frames, sink_frames, sink_attend, info.sm_count,
                      info.clusters[q8]);
     if (rc != UNSTEP_OK) return rc;
-    Workspace ws;
-    rc = scratch(st, 2 * static_cast<size_t>(info.sm_count), 2 * static_cast<size_t>(nb) * p.items_per_stream, &ws);
+    rc = bind_scratch(p, st, scratch, info.sm_count, out, 0);
     if (rc != UNSTEP_OK) return rc;
-    p.part = ws.part;
-    p.counters = ws.counters;
-    p.status = status_word();
-    p.out_wide = (reinterpret_cast<uintptr_t>(out) & 31u) == 0;   // rows are multiples of 256 bytes
-    p.extent_out = static_cast<int64_t>(nb) * p.L * p.Hn * (kHeadDim / 8);
-    p.extent_part = static_cast<int64_t>(ws.slots) * kPartFloats;
-    p.extent_counters = static_cast<int64_t>(ws.n_counters);
     const char* qb = static_cast<const char*>(q_rot) + static_cast<uint64_t>(b0) * L * row_bytes;
     const char* kb = static_cast<const char*>(ring_k) + static_cast<uint64_t>(b0) * C * T * cache_row_bytes;
     const char* vb = static_cast<const char*>(ring_v) + static_cast<uint64_t>(b0) * C * T * cache_row_bytes;
@@ -1228,27 +1351,12 @@ static int window_attn_run(const unstep_shape_t* shape, const int32_t* start_fra
     } else if (!make_map(&tm_k, kb, 5, rdims, rstr, 2) || !make_map(&tm_v, vb, 5, rdims, rstr, 2)) {
       return UNSTEP_ERR_CUDA;
     }
-    // Set up under the append before it where the launch is short.  Append and attention (with the pipeline of one
-    // S per query tile, 10 % slower per step), us not
-    // overlapped -> overlapped, by steps per worker: in runs of 20 (full clock) 24: 78.9 -> 76.5, 35:
-    // 94.6 -> 92.6, 57: 143.1 -> 142.3, 114: 242.0 -> 240.6, 226: 446.1 -> 445.5, 394: 754.9 -> 763.7; run
-    // on end at the power cap 24: 80.2 -> 79.8 (1912 -> 1867 MHz), 57: 155.2 -> 155.8 (1792 -> 1776), 114:
-    // 276.7 -> 276.6 (1702 -> 1688), 169: 395.4 -> 398.6 (1680 -> 1652), 394: 880.4 -> 895.9 (1635 -> 1605).
-    // The overlap saves 1.5-6 thousand cycles of a launch at any length; at the cap the clock falls for
-    // the idling it takes away.  The line lies about where the gain of short runs (0.6 % at 57 steps) has
-    // come down to the loss of runs at the cap (0.4 %).
-    const bool brief = p.all_steps < static_cast<int64_t>(kOverlapSteps) * p.n_workers;
-    const cudaError_t err =
-        launch_clusters(brief, p.cluster ? p.parts : 1,
-                        q8 ? (p.cluster ? window_attn_kernel<true, true> : window_attn_kernel<false, true>)
-                           : (p.cluster ? window_attn_kernel<true, false> : window_attn_kernel<false, false>),
-                        p.n_workers, q8 ? Form<true>::kThreads : Form<false>::kThreads, kAttnSmemBytes, st, tm_q, tm_k, tm_v,
-                        tm_kf, tm_vf, p, ob);
-    g_launches.fetch_add(1);
-    if (err != cudaSuccess) return UNSTEP_ERR_CUDA;
+    rc = launch_attn(p, q8, tm_q, tm_k, tm_v, tm_kf, tm_vf, ob, st);
+    if (rc != UNSTEP_OK) return rc;
   }
   return UNSTEP_OK;
 }
+
 
 #ifdef UNSTEP_TRACE
 extern "C" int unstep_debug_read_cta_trace(unsigned long long* host_out) {
@@ -1278,6 +1386,105 @@ extern "C" int unstep_window_attn_sink(const unstep_shape_t* shape, int32_t sink
                          get_workspace, sink_frames, sink_attend);
 }
 
+// Query-tile pairs of a head from which on the window of an 8-bit cache is unpacked in front of the attention.
+constexpr int kUnpackPairs = 5;
+
+// Attention over an 8-bit cache by way of unpacked windows, as many heads at a time as the scratch holds.  Leaves `done`
+// false where the kernel that decodes for itself is to do it.  Every tile of a head is decoded once here, and by each
+// query pair of the head there, next to a softmax that needs the issue slots.
+static int window_attn_unpacked(const unstep_shape_t* shape, int32_t sink_frames, const int32_t* start_frame,
+                                int32_t window_frames, int32_t sink_attend, const void* q_rot, const void* cache_k,
+                                const void* scale_k, const void* cache_v, const void* scale_v, void* out, cudaStream_t st,
+                                bool* done) {
+  int rc = check_attn_args(shape, start_frame, window_frames, sink_frames, sink_attend, true);
+  if (rc != UNSTEP_OK) return rc;
+  AttnParams p;
+  plan_shape(p, shape, sink_frames);
+  if (p.q_pairs < kUnpackPairs) return UNSTEP_OK;
+  const void* ptrs[] = {q_rot, cache_k, cache_v, out};
+  for (const void* ptr : ptrs)
+    if (ptr == nullptr || !aligned16(ptr)) return UNSTEP_ERR_INVALID_ARG;
+  rc = check_device();
+  if (rc != UNSTEP_OK) return rc;
+  const DeviceInfo& info = device_info();
+  if (!info.ok) return UNSTEP_ERR_CUDA;
+
+  const int64_t Hn = p.Hn, L = p.L, cache_rows = (static_cast<int64_t>(p.C) + sink_frames) * p.T;
+  const int64_t row_bytes = Hn * kHeadDim * 2;
+  p.flat = p.padded = 1;
+  // the widest window decides how many streams and heads go together
+  int64_t rows = 0;
+  for (int b = 0; b < shape->batch; ++b) {
+    const int64_t hi = static_cast<int64_t>(start_frame[b]) + shape->chunk_frames, lo = hi > window_frames ? hi - window_frames : 0;
+    const int64_t keys = ((sink_attend < lo ? sink_attend : lo) + hi - lo) * p.T;
+    rows = keys > rows ? keys : rows;
+  }
+  rows = (rows + kTileN - 1) / kTileN * kTileN;
+  const int64_t per_head = 2 * rows * kHeadDim * 2, room = static_cast<int64_t>(kMostWindow) / per_head;
+  if (room < 1) return UNSTEP_OK;
+  int64_t streams = shape->batch < kMaxStreamsPerLaunch ? shape->batch : kMaxStreamsPerLaunch;
+  if (streams > room) streams = room;
+  int64_t heads = room / streams < Hn ? room / streams : Hn;
+  heads = (Hn + (Hn + heads - 1) / heads - 1) / ((Hn + heads - 1) / heads);   // groups of equal size
+  uint8_t* const window = static_cast<uint8_t*>(get_window(st, streams * heads * per_head));
+  if (window == nullptr) return UNSTEP_OK;
+
+  for (int64_t b0 = 0; b0 < shape->batch; b0 += streams) {
+    const int nb = static_cast<int>(shape->batch - b0 < streams ? shape->batch - b0 : streams);
+    plan_windows(p, shape, start_frame + b0, nb, window_frames, sink_frames, sink_attend);
+    Unpack8Params u;
+    u.Hn = p.Hn;
+    u.rows = static_cast<int32_t>(rows);
+    u.cache_rows = cache_rows;
+    u.status = status_word();
+    for (int i = 0; i < nb; ++i) {
+      int32_t end = 0;
+      for (int r = 0; r < 3; ++r) {
+        u.run_row0[i][r] = p.run_row0[i][r];
+        u.run_end[i][r] = end += p.run_rows[i][r];
+      }
+      p.tiles[i] = (end + kTileN - 1) / kTileN;
+      for (int r = 0; r < 3; ++r) {   // one run, from the first row on
+        p.run_row0[i][r] = 0;
+        p.run_rows[i][r] = r == 0 ? end : 0;
+        p.run_tile_end[i][r] = p.tiles[i];
+      }
+    }
+    for (int64_t h0 = 0; h0 < Hn; h0 += heads) {
+      const int64_t g = Hn - h0 < heads ? Hn - h0 : heads;
+      p.items_per_stream = static_cast<int32_t>(g) * p.q_pairs;
+      plan_split(p, info.sm_count, info.clusters[0]);
+      uint8_t* const window_v = window + nb * g * rows * kHeadDim * 2;
+      u.head0 = static_cast<int32_t>(h0);
+      u.extent = nb * g * rows * (kHeadDim / 8);
+      const dim3 grid(static_cast<unsigned>((rows + 32 * kUnpackRows - 1) / (32 * kUnpackRows)), static_cast<unsigned>(g), nb);
+      const int64_t row0 = b0 * cache_rows * Hn;
+      const cudaError_t err = launch_overlapped(
+          true, window_unpack_q8_kernel, grid, 256, 0, st, u, static_cast<const uint4*>(cache_k) + row0 * 8,
+          static_cast<const uint8_t*>(scale_k) + row0 * 4, static_cast<const uint4*>(cache_v) + row0 * 8,
+          static_cast<const uint8_t*>(scale_v) + row0 * 4, reinterpret_cast<uint4*>(window), reinterpret_cast<uint4*>(window_v));
+      g_launches.fetch_add(1);
+      if (err != cudaSuccess) return UNSTEP_ERR_CUDA;
+      const char* qb = static_cast<const char*>(q_rot) + b0 * L * row_bytes + h0 * kHeadDim * 2;
+      char* ob = static_cast<char*>(out) + b0 * L * row_bytes + h0 * kHeadDim * 2;
+      rc = bind_scratch(p, st, get_workspace, info.sm_count, ob, h0 * (kHeadDim / 8));
+      if (rc != UNSTEP_OK) return rc;
+      CUtensorMap tm_q, tm_k, tm_v;
+      const uint64_t qdims[4] = {kHeadDim, static_cast<uint64_t>(g), static_cast<uint64_t>(L), static_cast<uint64_t>(nb)};
+      const uint64_t qstr[3] = {kHeadDim * 2, static_cast<uint64_t>(row_bytes), static_cast<uint64_t>(L * row_bytes)};
+      const uint64_t wdims[4] = {kHeadDim, static_cast<uint64_t>(g), static_cast<uint64_t>(rows), static_cast<uint64_t>(nb)};
+      const uint64_t wstr[3] = {static_cast<uint64_t>(rows) * kHeadDim * 2, kHeadDim * 2, static_cast<uint64_t>(g * rows) * kHeadDim * 2};
+      if (!make_map(&tm_q, qb, 4, qdims, qstr, 2) || !make_map(&tm_k, window, 4, wdims, wstr, 2) ||
+          !make_map(&tm_v, window_v, 4, wdims, wstr, 2))
+        return UNSTEP_ERR_CUDA;
+      rc = launch_attn(p, false, tm_q, tm_k, tm_v, tm_k, tm_v, reinterpret_cast<__nv_bfloat16*>(ob), st);
+      if (rc != UNSTEP_OK) return rc;
+    }
+  }
+  *done = true;
+  return UNSTEP_OK;
+}
+
 extern "C" int unstep_window_attn_q8(const unstep_shape_t* shape, int32_t sink_frames, const int32_t* start_frame,
                                      int32_t recent_frames, int32_t sink_attend, const void* q_rot, const void* cache_k,
                                      const void* scale_k, const void* cache_v, const void* scale_v, void* out,
@@ -1285,6 +1492,10 @@ extern "C" int unstep_window_attn_q8(const unstep_shape_t* shape, int32_t sink_f
   if (scale_k == nullptr || scale_v == nullptr || (reinterpret_cast<uintptr_t>(scale_k) & 3u) != 0 ||
       (reinterpret_cast<uintptr_t>(scale_v) & 3u) != 0)
     return UNSTEP_ERR_INVALID_ARG;
+  bool done = false;
+  const int rc = window_attn_unpacked(shape, sink_frames, start_frame, recent_frames, sink_attend, q_rot, cache_k, scale_k,
+                                      cache_v, scale_v, out, static_cast<cudaStream_t>(cuda_stream), &done);
+  if (rc != UNSTEP_OK || done) return rc;
   return window_attn_run(shape, start_frame, recent_frames, q_rot, cache_k, cache_v, out, cuda_stream,
                          get_workspace, sink_frames, sink_attend, scale_k, scale_v);
 }
@@ -1436,6 +1647,8 @@ extern "C" void unstep_shutdown(void) {
     if (s.ws.part != nullptr) cudaFree(s.ws.part);
     if (s.ws.counters != nullptr) cudaFree(s.ws.counters);
     for (int i = 0; i < s.n_left; ++i) cudaFree(s.left[i].counters);
+    for (void* window : s.window)
+      if (window != nullptr) cudaFree(window);
   }
   g_workspaces.clear();
   cudaSetDevice(cur);

@@ -28,6 +28,7 @@ struct AttnParams {
   int32_t q_pairs;          // ceil(q_tiles / 2)
   int32_t tiles_per_frame;  // ceil(T / 128)
   int32_t flat;             // 1: key tiles run across frame boundaries inside a slot run
+  int32_t padded;           // 1 (flat): what lies behind a run inside its last tile is finite, so that tile needs no zero fill
   int32_t n_streams;
   float scale_log2e;        // log2(e) / sqrt(128)
   int32_t items_per_stream; // Hn * q_pairs
@@ -93,7 +94,7 @@ UNSTEP_HD TileInfo tile_info(const AttnParams& p, int b, int j) {
     const int ntl = p.run_tile_end[b][r] - t_begin;
     const bool last = (tt == ntl - 1);
     t.valid = last ? rows - kTileN * tt : kTileN;
-    t.framed = last;
+    t.framed = last && !p.padded;
     t.row = row0 + kTileN * tt;
     t.slot = (row0 + rows - 1) / p.T;
     t.tok0 = p.T - t.valid;
@@ -301,14 +302,11 @@ inline int32_t cluster_parts(const AttnParams& p, int64_t items, int64_t steps, 
   return best;
 }
 
-// Fills the per-launch part of `p` for streams [b0, b0 + nb): the attended frames of each stream
-// cut into runs of consecutive cache slots, the key tiles, and the split of the work over at
-// most `max_workers` workers.  The shape-wide fields (Hn, L, T, C, q_tiles, q_pairs,
-// tiles_per_frame, flat, items_per_stream, sink) must already be set.  `clusters` as in cluster_parts;
-// without it no part is in a cluster.  Host only.
-inline int plan_launch(AttnParams& p, const unstep_shape_t* shape, const int32_t* start_frame, int nb,
-                       int32_t window_frames, int32_t sink_frames, int32_t sink_attend, int max_workers,
-                       const int32_t* clusters = nullptr) {
+// Fills the windows of streams [b0, b0 + nb) in `p`: the attended frames of each stream cut into runs of
+// consecutive cache slots, and the key tiles.  The shape-wide fields (L, T, C, tiles_per_frame, flat, sink) must
+// already be set.  Host only.
+inline void plan_windows(AttnParams& p, const unstep_shape_t* shape, const int32_t* start_frame, int nb,
+                         int32_t window_frames, int32_t sink_frames, int32_t sink_attend) {
   p.n_streams = nb;
   for (int i = 0; i < nb; ++i) {
     const int hi = start_frame[i] + shape->chunk_frames;
@@ -346,6 +344,12 @@ inline int plan_launch(AttnParams& p, const unstep_shape_t* shape, const int32_t
       p.tiles[i] = (n_sink + hi - lo) * p.tiles_per_frame;
     }
   }
+}
+
+// Splits the work of a launch whose windows are set over at most `max_workers` workers.  `clusters` as in
+// cluster_parts; without it no part is in a cluster.  Host only.
+inline void plan_split(AttnParams& p, int max_workers, const int32_t* clusters = nullptr) {
+  const int nb = p.n_streams;
   // One worker per SM where there are whole rounds for all of them; a launch of fewer items than
   // that is all remainder, and has the workers that the split asks for.
   const int64_t all_items = static_cast<int64_t>(nb) * p.items_per_stream;
@@ -378,6 +382,14 @@ inline int plan_launch(AttnParams& p, const unstep_shape_t* shape, const int32_t
     p.narrow = steps * p.n_active <= INT32_MAX;
     if (p.full_rounds == 0) p.n_workers = p.parts > 0 ? static_cast<int32_t>(items) * p.parts : p.n_active;
   }
+}
+
+// Both.  The shape-wide fields must already be set.
+inline int plan_launch(AttnParams& p, const unstep_shape_t* shape, const int32_t* start_frame, int nb,
+                       int32_t window_frames, int32_t sink_frames, int32_t sink_attend, int max_workers,
+                       const int32_t* clusters = nullptr) {
+  plan_windows(p, shape, start_frame, nb, window_frames, sink_frames, sink_attend);
+  plan_split(p, max_workers, clusters);
   return UNSTEP_OK;
 }
 
@@ -394,6 +406,7 @@ inline void plan_shape(AttnParams& p, const unstep_shape_t* shape, int32_t sink_
   p.q_pairs = (p.q_tiles + 1) / 2;
   p.tiles_per_frame = static_cast<int32_t>((T + kTileN - 1) / kTileN);
   p.flat = (T >= kTileN) ? 1 : 0;  // a ragged tile must fit inside one frame
+  p.padded = 0;
   p.scale_log2e = 1.4426950408889634f / 11.313708498984761f;   // log2(e) / sqrt(128)
   p.items_per_stream = p.Hn * p.q_pairs;
   p.part = nullptr;

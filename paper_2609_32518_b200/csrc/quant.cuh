@@ -45,12 +45,12 @@ __device__ __forceinline__ uint2 quantise8(const float* y, uint32_t* byte) {
   return make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
 }
 
-// Two codes of a word (its lower or upper half) as bf16 of 2^-120 times their value: exponent and mantissa of
-// e4m3, moved to the lowest exponent bits of bf16, subnormals included.
-template <int kHalf>
-__device__ __forceinline__ uint32_t spread(uint32_t w) {
-  const uint32_t x = __byte_perm(w, 0u, kHalf ? 0x3424 : 0x1404);
-  return ((x >> 4) & 0x07F007F0u) | (x & 0x80008000u);
+// Four codes as two bf16 pairs of 2^-120 times their values: exponent and mantissa of e4m3, moved to the lowest exponent
+// bits of bf16, subnormals included.  The upper bytes of the four bf16 (sign, three exponent bits) and the lower ones
+// are made four at a time.
+__device__ __forceinline__ uint2 spread4(uint32_t w) {
+  const uint32_t upper = (w & 0x80808080u) | ((w >> 4) & 0x07070707u), lower = (w << 4) & 0xF0F0F0F0u;
+  return make_uint2(__byte_perm(lower, upper, 0x5140), __byte_perm(lower, upper, 0x7362));
 }
 __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
   const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
@@ -67,8 +67,8 @@ __device__ __forceinline__ uint32_t factor2(uint32_t byte) {
 
 // 8 codes (two words) as 8 bf16.
 __device__ __forceinline__ uint4 decode8(uint32_t w0, uint32_t w1, uint32_t f1) {
-  return make_uint4(mul_bf16x2(spread<0>(w0), f1), mul_bf16x2(spread<1>(w0), f1), mul_bf16x2(spread<0>(w1), f1),
-                    mul_bf16x2(spread<1>(w1), f1));
+  const uint2 a = spread4(w0), b = spread4(w1);
+  return make_uint4(mul_bf16x2(a.x, f1), mul_bf16x2(a.y, f1), mul_bf16x2(b.x, f1), mul_bf16x2(b.y, f1));
 }
 __device__ __forceinline__ uint4 mul8(uint4 x, uint32_t f) {
   return make_uint4(mul_bf16x2(x.x, f), mul_bf16x2(x.y, f), mul_bf16x2(x.z, f), mul_bf16x2(x.w, f));

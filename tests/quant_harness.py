@@ -55,6 +55,16 @@ class Layer:
         self.ora.cache_v, self.ora.scale_v = Q.quantise(v)
         self.upload()
 
+    def fill_codes(self, seed: int):
+        """Random codes and scales in every slot, values below 1: large caches, quickly."""
+        rng = np.random.default_rng(seed)
+        for c, e in (("cache_k", "scale_k"), ("cache_v", "scale_v")):
+            codes = rng.integers(0, 256, getattr(self.ora, c).shape, dtype=np.uint8)
+            codes[(codes & 127) == 127] = 0
+            setattr(self.ora, c, codes)
+            setattr(self.ora, e, rng.integers(114, 119, getattr(self.ora, e).shape, dtype=np.uint8))
+        self.upload()
+
     def tables(self, starts):
         sh = self.sh
         t = [Q.rotary_table(int(s), sh.chunk_frames, sh.grid_h, sh.grid_w, self.bands, self.rope) for s in starts]

@@ -244,6 +244,88 @@ def test_attention(name):
         q = q.flip(1).contiguous()
 
 
+# From five pairs of query tiles on the window is unpacked first.
+UNPACKED = [
+    ("1025_queries", (1, 2, (5, 205), 1, 2, 0, 2, 0, (3,))),
+    ("small_frames_wrapped", (2, 3, (7, 9), 20, 23, 1, 21, 1, (80, 20))),
+    ("sink_and_ring_wrapped", (2, 2, (20, 21), 3, 6, 3, 6, 2, (13, 6))),
+    ("first_chunk", (3, 2, (20, 21), 3, 6, 3, 6, 3, (0, 3, 1))),
+    ("34_streams", (34, 1, (11, 100), 1, 2, 0, 2, 0, tuple(b % 4 for b in range(34)))),
+]
+
+
+@pytest.mark.parametrize("name", [n for n, _ in UNPACKED])
+def test_attention_over_unpacked_windows(name):
+    batch, heads, grid, fc, ring, sink, recent, attend, starts = dict(UNPACKED)[name]
+    sh = shape(batch, heads, fc, *grid, ring)
+    layer = Layer(sh, sink)
+    layer.fill_codes(50)
+    q = layer.queries(51)
+    rows = W.sample_rows(sh.chunk_tokens)
+    for rep in range(2):
+        launches = U.launch_count()
+        got = layer.attend(starts, recent, attend, q)
+        assert U.launch_count() - launches == 2 * ((batch + 31) // 32)
+        check(got[:, rows], layer.attend_oracle(starts, recent, attend, q, rows=rows), f"{name} {rep}")
+        layer.fill_codes(52)                                      # the scratch holds the former window
+    assert U.poll_status() == 0
+
+
+def test_heads_in_groups_where_the_unpacked_windows_exceed_the_scratch():
+    # 40 heads x 13 200 keys x 512 bytes are 270 MB: two groups of 20 heads; and streams one by one
+    for batch, heads, frames in ((1, 40, 12), (2, 17, 12)):
+        sh = shape(batch, heads, 1, 11, 100, frames)
+        layer = Layer(sh)
+        layer.fill_codes(53)
+        q = layer.queries(54)
+        starts = [frames + 3 + b for b in range(batch)]
+        launches = U.launch_count()
+        got = layer.attend(starts, frames, 0, q)
+        assert U.launch_count() - launches == 4
+        rows, some = W.sample_rows(sh.chunk_tokens)[::4], sorted({0, heads // 2 - 1, heads // 2, heads - 1})
+        check(got[:, rows][:, :, some], layer.attend_oracle(starts, frames, 0, q, rows=rows, heads=some), f"{heads} heads")
+    assert U.poll_status() == 0
+
+
+def test_unpacked_window_of_a_captured_graph_survives_larger_calls():
+    small, large = Layer(shape(1, 2, 1, 11, 100, 2)), Layer(shape(1, 4, 1, 11, 100, 9))
+    for layer, seed in ((small, 55), (large, 56)):
+        layer.fill_codes(seed)
+    q, q_large = small.queries(57), large.queries(58)
+    side = torch.cuda.Stream()
+    out, want = torch.zeros_like(q), torch.zeros_like(q)
+    torch.cuda.synchronize()
+
+    def call(layer, x, o, start, n):
+        U.window_attn_q8(layer.abi, 0, [start], n, 0, x, *layer.cache, o, stream=side)
+
+    call(small, q, want, 4, 2)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        call(small, q, out, 4, 2)
+    call(large, q_large, torch.empty_like(q_large), 11, 9)        # a larger scratch on the same stream
+    side.synchronize()
+    for _ in range(2):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out.view(torch.int16), want.view(torch.int16))
+    # a capture on a stream that has no scratch yet decodes inside the attention, within the bounds
+    fresh, other = torch.cuda.Stream(), torch.zeros_like(q)
+    few = Layer(shape(1, 2, 1, 1, 1, 2))
+    few.fill_codes(59)
+    q_few = few.queries(60)
+    torch.cuda.synchronize()
+    U.window_attn_q8(few.abi, 0, [4], 2, 0, q_few, *few.cache, torch.empty_like(q_few), stream=fresh)   # counters
+    graph2 = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph2, stream=fresh):
+        U.window_attn_q8(small.abi, 0, [4], 2, 0, q, *small.cache, other, stream=fresh)
+    graph2.replay()
+    torch.cuda.synchronize()
+    check(other, small.attend_oracle([4], 2, 0, q), "captured without scratch")
+    assert U.poll_status() == 0
+
+
 def test_attention_leaves_what_it_does_not_attend_alone():
     # every slot outside the window holds NaN blocks, and codes that nobody writes
     sh = shape(2, 2, 2, 3, 19, 8)
