@@ -1107,7 +1107,7 @@ static DeviceInfo query_device(int dev) {
   if (it != known.end()) return it->second;
   DeviceInfo info;
   info.ok = cudaDeviceGetAttribute(&info.sm_count, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess &&
-            query_kernels<false>(info.clusters[0]) && query_kernels<true>(info.clusters[1]);
+            query_kernels<false>(info.clusters[0]) && query_kernels<true>(info.clusters[1]) && few_setup();
   if (!info.ok) return info;
   return known[dev] = info;
 }
@@ -1389,10 +1389,10 @@ extern "C" int unstep_window_attn_sink(const unstep_shape_t* shape, int32_t sink
 // Query-tile pairs of a head from which on the window of an 8-bit cache is unpacked in front of the attention.
 constexpr int kUnpackPairs = 5;
 
-// Attention over an 8-bit cache by way of unpacked windows, as many heads at a time as the scratch holds.  Leaves `done`
-// false where the kernel that decodes for itself is to do it.  Every tile of a head is decoded once here, and by each
-// query pair of the head there, next to a softmax that needs the issue slots.
-static int window_attn_unpacked(const unstep_shape_t* shape, int32_t sink_frames, const int32_t* start_frame,
+// Attention over an 8-bit cache with few queries, or with many, by way of unpacked windows, as many heads at a time as the
+// scratch holds.  Leaves `done` false where the kernel that decodes tiles for itself is to do it.  With many queries every
+// tile of a head is decoded once here, and by each query pair of the head there, next to a softmax that needs the issue slots.
+static int window_attn_q8_run(const unstep_shape_t* shape, int32_t sink_frames, const int32_t* start_frame,
                                 int32_t window_frames, int32_t sink_attend, const void* q_rot, const void* cache_k,
                                 const void* scale_k, const void* cache_v, const void* scale_v, void* out, cudaStream_t st,
                                 bool* done) {
@@ -1400,7 +1400,7 @@ static int window_attn_unpacked(const unstep_shape_t* shape, int32_t sink_frames
   if (rc != UNSTEP_OK) return rc;
   AttnParams p;
   plan_shape(p, shape, sink_frames);
-  if (p.q_pairs < kUnpackPairs) return UNSTEP_OK;
+  if (p.L > kFewQueries && p.q_pairs < kUnpackPairs) return UNSTEP_OK;
   const void* ptrs[] = {q_rot, cache_k, cache_v, out};
   for (const void* ptr : ptrs)
     if (ptr == nullptr || !aligned16(ptr)) return UNSTEP_ERR_INVALID_ARG;
@@ -1412,6 +1412,20 @@ static int window_attn_unpacked(const unstep_shape_t* shape, int32_t sink_frames
   const int64_t Hn = p.Hn, L = p.L, cache_rows = (static_cast<int64_t>(p.C) + sink_frames) * p.T;
   const int64_t row_bytes = Hn * kHeadDim * 2;
   p.flat = p.padded = 1;
+  p.cache_rows = cache_rows;
+  if (p.L <= kFewQueries) {
+    for (int64_t b0 = 0; b0 < shape->batch; b0 += kMaxStreamsPerLaunch) {
+      const int nb = static_cast<int>(shape->batch - b0 < kMaxStreamsPerLaunch ? shape->batch - b0 : kMaxStreamsPerLaunch);
+      plan_windows(p, shape, start_frame + b0, nb, window_frames, sink_frames, sink_attend);
+      const int64_t act = b0 * L * row_bytes, rows = b0 * cache_rows * Hn;
+      rc = launch_few(p, nb, info.sm_count, static_cast<const char*>(q_rot) + act, static_cast<const char*>(cache_k) + rows * kHeadDim,
+                      static_cast<const char*>(scale_k) + rows * 4, static_cast<const char*>(cache_v) + rows * kHeadDim,
+                      static_cast<const char*>(scale_v) + rows * 4, static_cast<char*>(out) + act, st);
+      if (rc != UNSTEP_OK) return rc;
+    }
+    *done = true;
+    return UNSTEP_OK;
+  }
   // the widest window decides how many streams and heads go together
   int64_t rows = 0;
   for (int b = 0; b < shape->batch; ++b) {
@@ -1493,7 +1507,7 @@ extern "C" int unstep_window_attn_q8(const unstep_shape_t* shape, int32_t sink_f
       (reinterpret_cast<uintptr_t>(scale_v) & 3u) != 0)
     return UNSTEP_ERR_INVALID_ARG;
   bool done = false;
-  const int rc = window_attn_unpacked(shape, sink_frames, start_frame, recent_frames, sink_attend, q_rot, cache_k, scale_k,
+  const int rc = window_attn_q8_run(shape, sink_frames, start_frame, recent_frames, sink_attend, q_rot, cache_k, scale_k,
                                       cache_v, scale_v, out, static_cast<cudaStream_t>(cuda_stream), &done);
   if (rc != UNSTEP_OK || done) return rc;
   return window_attn_run(shape, start_frame, recent_frames, q_rot, cache_k, cache_v, out, cuda_stream,

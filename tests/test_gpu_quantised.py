@@ -213,6 +213,7 @@ def check(got: torch.Tensor, ref, what):
 ATTN = [
     # batch, heads, grid, chunk, ring, sink, recent, sink_attend, starts
     ("one_key", (1, 1, (1, 1), 1, 1, 0, 1, 0, (0,))),
+    ("17_queries_33_keys", (1, 3, (1, 17), 1, 2, 0, 2, 0, (50,))),
     ("one_query_37_keys", (1, 3, (1, 1), 1, 37, 0, 37, 0, (50,))),
     ("tokens", (3, 5, (1, 1), 1, 700, 2, 650, 2, (1500, 3, 699))),
     ("127_keys", (1, 2, (1, 127), 1, 1, 0, 1, 0, (4,))),
@@ -242,6 +243,51 @@ def test_attention(name):
         check(got[:, :, some], layer.attend_oracle(starts, recent, attend, q, heads=some), f"{name} {rep}")
         assert U.poll_status() == 0
         q = q.flip(1).contiguous()
+
+
+# Up to 16 queries a stream: keys go straight from memory into warp-level products.
+FEW = [
+    ("8_queries_one_key", (1, 1, (1, 8), 1, 1, 0, 1, 0, (0,))),
+    ("9_queries", (2, 3, (3, 3), 1, 40, 2, 33, 1, (100, 7))),
+    ("16_queries_wrapped", (1, 5, (2, 4), 2, 30, 0, 29, 0, (77,))),
+    ("15_keys", (1, 2, (1, 3), 1, 5, 0, 5, 0, (9,))),
+    ("17_keys", (2, 2, (1, 1), 1, 17, 0, 17, 0, (40, 16))),
+    ("34_streams", (34, 3, (1, 2), 1, 90, 1, 70, 1, tuple(3 * b for b in range(34)))),
+    ("long", (1, 1, (1, 1), 1, 9001, 0, 9001, 0, (20000,))),
+    ("many_items", (3, 40, (1, 1), 1, 200, 0, 200, 0, (300, 10, 199))),
+    ("no_scratch_queries_17", (1, 2, (1, 17), 1, 9, 0, 9, 0, (20,))),
+]
+
+
+@pytest.mark.parametrize("name", [n for n, _ in FEW])
+@pytest.mark.parametrize("v_power", [0, 60])
+def test_attention_of_few_queries(name, v_power):
+    batch, heads, grid, fc, ring, sink, recent, attend, starts = dict(FEW)[name]
+    sh = shape(batch, heads, fc, *grid, ring)
+    layer = Layer(sh, sink)
+    layer.fill(70, k_scale=2.0, v_power=v_power)
+    q = layer.queries(71)
+    got, ref = layer.attend(starts, recent, attend, q), layer.attend_oracle(starts, recent, attend, q)
+    if v_power == 0:
+        check(got, ref, name)
+    got = got.double().cpu().numpy()
+    assert np.isfinite(got).all() and np.linalg.norm(got - ref) <= REL_L2 * np.linalg.norm(ref)
+    assert U.poll_status() == 0
+
+
+def test_few_queries_of_peaked_keys_in_rising_order():
+    # every step of a warp has a larger maximum than the one before: sums and results are rescaled each time
+    sh = shape(1, 2, 1, 1, 2, 700)
+    layer = Layer(sh)
+    rng = np.random.default_rng(72)
+    k = rng.standard_normal(layer.ora.cache_k.shape).astype(np.float32)
+    k[..., 0] = np.linspace(0, 200, 700, dtype=np.float32)[None, :, None, None]
+    layer.ora.cache_k, layer.ora.scale_k = Q.quantise(k)
+    layer.ora.cache_v, layer.ora.scale_v = Q.quantise(rng.standard_normal(k.shape).astype(np.float32))
+    layer.upload()
+    q = layer.queries(73)
+    q[..., 0] = 3.0
+    check(layer.attend([699], 700, 0, q), layer.attend_oracle([699], 700, 0, q), "rising")
 
 
 # From five pairs of query tiles on the window is unpacked first.
@@ -312,7 +358,7 @@ def test_unpacked_window_of_a_captured_graph_survives_larger_calls():
         assert torch.equal(out.view(torch.int16), want.view(torch.int16))
     # a capture on a stream that has no scratch yet decodes inside the attention, within the bounds
     fresh, other = torch.cuda.Stream(), torch.zeros_like(q)
-    few = Layer(shape(1, 2, 1, 1, 1, 2))
+    few = Layer(shape(1, 2, 1, 4, 10, 2))
     few.fill_codes(59)
     q_few = few.queries(60)
     torch.cuda.synchronize()

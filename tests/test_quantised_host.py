@@ -164,14 +164,14 @@ def test_native_marshalling_answers_none_for_what_is_not_well_formed():
 
 
 def test_inputs_of_overlapped_kernels_are_read_behind_the_wait():
-    found = list(kernels("rotary.cu"))
-    assert len(found) == 3
+    found = list(kernels("rotary.cu")) + list(kernels("attn_few.cu"))
+    assert len(found) == 4
     for name, params, body in found:
         assert "grid_wait()" in body, name
         assert not re.search(r"const\s+(?!__grid_constant__)\w+\s*\*\s*__restrict__", params), name
         assert "__ldg(" not in body, name
         wait = body.index("grid_wait()")
-        for load in re.finditer(r"__ldca\(|__ldcs\(|q_in\[|load_coefficients", body):
+        for load in re.finditer(r"__ldca\(|__ldcs\(|q_in\[|= load_coefficients", body):
             assert load.start() > wait, name
         # addresses take the wait's zero in
         assert re.search(r"\+ behind|\+= behind", body), name
