@@ -1073,6 +1073,7 @@ struct DeviceInfo {
   int sm_count = 0;
   int32_t clusters[2][kMaxClusterParts + 1] = {};   // clusters of that many blocks which the device runs at the same
                                                     // time, of the kernel over a bf16 and of that over an 8-bit cache
+  int32_t few_blocks[2] = {};   // blocks of the kernel for few queries that an SM holds
 };
 
 template <bool kQ8>
@@ -1107,7 +1108,7 @@ static DeviceInfo query_device(int dev) {
   if (it != known.end()) return it->second;
   DeviceInfo info;
   info.ok = cudaDeviceGetAttribute(&info.sm_count, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess &&
-            query_kernels<false>(info.clusters[0]) && query_kernels<true>(info.clusters[1]) && few_setup();
+            query_kernels<false>(info.clusters[0]) && query_kernels<true>(info.clusters[1]) && few_setup(info.few_blocks);
   if (!info.ok) return info;
   return known[dev] = info;
 }
@@ -1417,8 +1418,11 @@ static int window_attn_q8_run(const unstep_shape_t* shape, int32_t sink_frames, 
     for (int64_t b0 = 0; b0 < shape->batch; b0 += kMaxStreamsPerLaunch) {
       const int nb = static_cast<int>(shape->batch - b0 < kMaxStreamsPerLaunch ? shape->batch - b0 : kMaxStreamsPerLaunch);
       plan_windows(p, shape, start_frame + b0, nb, window_frames, sink_frames, sink_attend);
+      p.items_per_stream = p.Hn;
+      rc = bind_scratch(p, st, get_workspace, info.sm_count, out, 0);
+      if (rc != UNSTEP_OK) return rc;
       const int64_t act = b0 * L * row_bytes, rows = b0 * cache_rows * Hn;
-      rc = launch_few(p, nb, info.sm_count, static_cast<const char*>(q_rot) + act, static_cast<const char*>(cache_k) + rows * kHeadDim,
+      rc = launch_few(p, nb, info.sm_count, info.few_blocks, static_cast<const char*>(q_rot) + act, static_cast<const char*>(cache_k) + rows * kHeadDim,
                       static_cast<const char*>(scale_k) + rows * 4, static_cast<const char*>(cache_v) + rows * kHeadDim,
                       static_cast<const char*>(scale_v) + rows * 4, static_cast<char*>(out) + act, st);
       if (rc != UNSTEP_OK) return rc;

@@ -7,7 +7,9 @@
 // The dims of K, summed over, and those of V, independent of each other, may come in any order, so every thread
 // reads 16 or 32 neighbouring codes of a row and needs no exchange; P^T turns from result to operand by a
 // transpose of its 8 x 8 blocks.  Each warp has its own running maximum and sum; the warps of a block merge through
-// shared memory, the blocks of an item (stream, head) are a cluster and merge through each other's.
+// shared memory, the blocks of an item (stream, head) through the scratch: the one that is done last reads the
+// others' parts, in part order, so the result does not depend on which one that is.  Streams of different length get
+// different numbers of blocks, which clusters could not have.
 #include <cuda_bf16.h>
 
 #include "attn_sched.h"
@@ -21,13 +23,19 @@ using namespace ptx;
 
 constexpr int kFewWarps = 8, kFewThreads = 32 * kFewWarps;
 constexpr int kFewKeys = 16;                    // keys of a warp's step
+constexpr int kFewParts = 64;                   // most blocks of an item
+constexpr float kFewJump = 57.f;                // as far (log2) a score may be above the reference, as in attn.cu
 
 struct FewParams {
-  int32_t Hn, L, parts;
+  int32_t Hn, L, n_streams;
+  int32_t wide;                                 // 1: cache_k is 32-byte aligned
   int64_t cache_rows;                           // rows of a stream's cache
   float scale_log2e;
+  float* part;                                  // scratch: part_floats for every block
+  int* counters;                                // scratch: arrivals per item, zero between launches
   int* status;
-  int64_t extent_out;                           // 4-byte words of `out`
+  int64_t extent_out, extent_part, extent_counters;   // 4-byte words of `out`, floats of `part`, ints of `counters`
+  int32_t parts[kMaxStreamsPerLaunch], block0[kMaxStreamsPerLaunch];   // blocks of an item of a stream, its first block
   int32_t run_row0[kMaxStreamsPerLaunch][3], run_end[kMaxStreamsPerLaunch][3];   // rows of the runs, added up
 };
 
@@ -42,48 +50,57 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
-// Four codes times their scale, as two bf16 pairs.
-__device__ __forceinline__ uint2 decode4(uint32_t w, uint32_t f1, uint32_t f2, bool two) {
-  uint2 y = q8::spread4(w);
-  y.x = q8::mul_bf16x2(y.x, f1);
-  y.y = q8::mul_bf16x2(y.y, f1);
-  if (two) {
-    y.x = q8::mul_bf16x2(y.x, f2);
-    y.y = q8::mul_bf16x2(y.y, f2);
-  }
-  return y;
+// Four codes as bf16 pairs, (0, 2) in x and (1, 3) in y, of 2^-120 times their values: without the bytes of q8::spread4
+// brought back in order, which is the caller's to choose here.
+__device__ __forceinline__ uint2 spread_pairs(uint32_t w) {
+  return make_uint2(((w << 8) & 0x80008000u) | ((w << 4) & 0x07F007F0u), (w & 0x80008000u) | ((w >> 4) & 0x07F007F0u));
 }
+// The multiplier of q8::factor1, for scale bytes up to 134.
+__device__ __forceinline__ uint32_t factor_small(uint32_t byte) { return byte * 0x00800080u + 120u * 0x00800080u; }
 
+// What a warp leaves in shared memory: O as [query][dim], then (m, l).
 template <int kN>   // groups of 8 queries
-constexpr int few_smem_bytes() {
-  return (kFewWarps * 8 * kN * kHeadDim + kFewWarps * 8 * kN * 2 + 8 * kN * kHeadDim + 8 * kN * 2) * static_cast<int>(sizeof(float));
+__host__ __device__ constexpr int few_warp_bytes() {
+  return 8 * kN * (kHeadDim + 2) * static_cast<int>(sizeof(float));
+}
+// A block's part in the scratch: O as [query][dim], then (m, l) as [query].
+template <int kN>
+__host__ __device__ constexpr int few_part_floats() {
+  return 8 * kN * kHeadDim + 8 * kN * 2;
 }
 
 template <int kN>
 __global__ void __launch_bounds__(kFewThreads, kN == 1 ? 2 : 1)
 window_attn_few_kernel(const __grid_constant__ FewParams p, const uint4* q_rot, const uint4* cache_k, const uint8_t* scale_k,
                        const uint4* cache_v, const uint8_t* scale_v, uint32_t* out) {
-  extern __shared__ __align__(16) float few_smem[];
-  float* const slabs = few_smem;                                        // [warp][query][dim]: O of a warp
-  float2* const warp_ml = reinterpret_cast<float2*>(slabs + kFewWarps * 8 * kN * kHeadDim);   // [warp][query]
-  float* const mine = reinterpret_cast<float*>(warp_ml + kFewWarps * 8 * kN);                 // [query][dim]: O of the block
-  float2* const my_ml = reinterpret_cast<float2*>(mine + 8 * kN * kHeadDim);                  // [query]
+  extern __shared__ __align__(16) uint8_t few_smem[];
+  auto slab = [&](int w, int query) { return reinterpret_cast<float*>(few_smem + w * few_warp_bytes<kN>()) + query * kHeadDim; };
+  auto slab_ml = [&](int w) { return reinterpret_cast<float2*>(slab(w, 8 * kN)); };
+  __shared__ int last;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
-  const int item = blockIdx.x / p.parts, part = blockIdx.x - item * p.parts;
-  const int b = item / p.Hn, h = item - b * p.Hn;
+  const int block = static_cast<int>(blockIdx.x);
+  int b = 0;
+  while (b + 1 < p.n_streams && p.block0[b + 1] <= block) ++b;
+  const int parts = p.parts[b], h = (block - p.block0[b]) / parts, part = block - p.block0[b] - h * parts;
   const int end0 = p.run_end[b][0], end1 = p.run_end[b][1], keys = p.run_end[b][2];
   const int row0 = p.run_row0[b][0], row1 = p.run_row0[b][1] - end0, row2 = p.run_row0[b][2] - end1;
   const int steps = (keys + kFewKeys - 1) / kFewKeys;
-  const int lo = static_cast<int>(static_cast<int64_t>(steps) * part / p.parts);
-  const int hi = static_cast<int>(static_cast<int64_t>(steps) * (part + 1) / p.parts);
-  const int64_t base = b * p.cache_rows;
-  // where key j lies, in rows of a head; keys behind the last are the last again, and masked
+  const int lo = static_cast<int>(static_cast<int64_t>(steps) * part / parts);
+  const int hi = static_cast<int>(static_cast<int64_t>(steps) * (part + 1) / parts);
+  // the row of key j in this stream's cache; keys behind the last are the last again, and masked
   auto row_of = [&](int j) {
     j = min(j, keys - 1);
-    return (base + (j < end0 ? row0 + j : (j < end1 ? row1 + j : row2 + j))) * p.Hn + h;
+    return static_cast<uint32_t>(j + (j < end0 ? row0 : (j < end1 ? row1 : row2)));
   };
-  const int behind = grid_wait();
+  // from here on everything is read, at addresses that take the wait's 0 in
+  const int64_t head = b * p.cache_rows * p.Hn + h + grid_wait();
+  const uint4* const head_k = cache_k + head * 8;
+  const uint4* const head_v = cache_v + head * 8;
+  const uint8_t* const head_ek = scale_k + head * 4;
+  const uint8_t* const head_ev = scale_v + head * 4;
+  const uint4* const head_q = q_rot + (b * (static_cast<int64_t>(p.L) - p.cache_rows) * p.Hn + head) * 16;
+  const uint32_t row_codes = 8u * p.Hn, row_scales = 4u * p.Hn;
 
   // B of S^T: thread (g, c) has query g, dims 32 c ..
   uint32_t q[kN][16];
@@ -93,8 +110,10 @@ window_attn_few_kernel(const __grid_constant__ FewParams p, const uint4* q_rot, 
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       uint4 x = make_uint4(0, 0, 0, 0);
-      if (query < p.L) x = __ldca(q_rot + ((static_cast<int64_t>(b) * p.L + query) * p.Hn + h) * 16 + 4 * c + i + behind);
-      q[n][4 * i] = x.x, q[n][4 * i + 1] = x.y, q[n][4 * i + 2] = x.z, q[n][4 * i + 3] = x.w;
+      if (query < p.L) x = __ldca(head_q + static_cast<int64_t>(query) * p.Hn * 16 + 4 * c + i);
+      // pairs (0, 2) and (1, 3) of four dims, as spread_pairs makes them
+      q[n][4 * i] = __byte_perm(x.x, x.y, 0x5410), q[n][4 * i + 1] = __byte_perm(x.x, x.y, 0x7632);
+      q[n][4 * i + 2] = __byte_perm(x.z, x.w, 0x5410), q[n][4 * i + 3] = __byte_perm(x.z, x.w, 0x7632);
     }
   }
   float o[kN][8][4];   // O^T: dims 16 g + 2 t and + 2 t + 1, queries 8 n + 2 c and + 1
@@ -107,26 +126,65 @@ window_attn_few_kernel(const __grid_constant__ FewParams p, const uint4* q_rot, 
     for (int t = 0; t < 8; ++t) o[n][t][0] = o[n][t][1] = o[n][t][2] = o[n][t][3] = 0.f;
   }
 
-  uint4 xk[2][2], xv[4];     // codes of keys g, g + 8 (dims 32 c ..) and of keys 2 c, 2 c + 1, 2 c + 8, 2 c + 9 (dims 16 g ..)
+  // codes of keys g, g + 8 (dims 32 c ..) and of keys 2 c, 2 c + 1, 2 c + 8, 2 c + 9 (dims 16 g ..), a step ahead
+  uint32_t xk[2][8];
+  uint4 xv[4];
   uint32_t ek[2], ev[4];
+  // A step whose keys lie in one run has its rows at fixed distances from the first one's; the others are looked up.
+  const uint32_t off_k = (g * row_codes + 2 * c) * 16, off_v = (2 * c * row_codes + g) * 16;
+  const uint32_t off_ek = g * row_scales + c, off_ev = 2 * c * row_scales + (g >> 1);
+  auto plain = [&](int step) {
+    const int j = step * kFewKeys, e = j + kFewKeys;
+    return j >= end1 ? e <= keys : (j >= end0 ? e <= end1 : e <= end0);
+  };
+  auto load_row = [&](const void* from, uint32_t* x) {   // 32 codes
+    if (p.wide) {
+      ld_global_32(from, x);
+    } else {
+      const uint4 a = __ldcs(static_cast<const uint4*>(from)), d = __ldcs(static_cast<const uint4*>(from) + 1);
+      x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = d.x, x[5] = d.y, x[6] = d.z, x[7] = d.w;
+    }
+  };
   auto load_k = [&](int step) {
+    if (__builtin_expect(plain(step), 1)) {
+      const uint64_t r = row_of(step * kFewKeys);
+      const char* const k0 = reinterpret_cast<const char*>(head_k + r * row_codes);
+      const uint8_t* const e0 = head_ek + r * row_scales;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int64_t r = row_of(step * kFewKeys + g + 8 * i) + behind;
-      xk[i][0] = __ldcs(cache_k + r * 8 + 2 * c);
-      xk[i][1] = __ldcs(cache_k + r * 8 + 2 * c + 1);
-      ek[i] = __ldca(scale_k + r * 4 + c);
+      for (int i = 0; i < 2; ++i) {
+        load_row(k0 + (off_k + 8 * i * row_codes * 16), xk[i]);
+        ek[i] = __ldca(e0 + (off_ek + 8 * i * row_scales));
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint64_t r = row_of(step * kFewKeys + g + 8 * i);
+        load_row(head_k + r * row_codes + 2 * c, xk[i]);
+        ek[i] = __ldca(head_ek + r * row_scales + c);
+      }
     }
   };
   auto load_v = [&](int step) {
+    if (__builtin_expect(plain(step), 1)) {
+      const uint64_t r = row_of(step * kFewKeys);
+      const char* const v0 = reinterpret_cast<const char*>(head_v + r * row_codes);
+      const uint8_t* const e0 = head_ev + r * row_scales;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int64_t r = row_of(step * kFewKeys + 2 * c + (i & 1) + 8 * (i >> 1)) + behind;
-      xv[i] = __ldcs(cache_v + r * 8 + g);
-      ev[i] = __ldca(scale_v + r * 4 + (g >> 1));
+      for (int i = 0; i < 4; ++i) {
+        xv[i] = __ldcs(reinterpret_cast<const uint4*>(v0 + (off_v + ((i & 1) + 8 * (i >> 1)) * row_codes * 16)));
+        ev[i] = __ldca(e0 + (off_ev + ((i & 1) + 8 * (i >> 1)) * row_scales));
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint64_t r = row_of(step * kFewKeys + 2 * c + (i & 1) + 8 * (i >> 1));
+        xv[i] = __ldcs(head_v + r * row_codes + g);
+        ev[i] = __ldca(head_ev + r * row_scales + (g >> 1));
+      }
     }
   };
   int step = lo + warp;
+  bool first = true;
   if (step < hi) {
     load_k(step);
     load_v(step);
@@ -136,42 +194,56 @@ window_attn_few_kernel(const __grid_constant__ FewParams p, const uint4* q_rot, 
     float s[kN][4];
 #pragma unroll
     for (int n = 0; n < kN; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+    // one factor up to a scale byte of 134, else 2^120 and another
+    const bool two_k = __any_sync(0xFFFFFFFFu, max(ek[0], ek[1]) > 134u);
     {
-      const bool two = __any_sync(0xFFFFFFFFu, !q8::one_factor(ek[0]) || !q8::one_factor(ek[1]));
-      const uint32_t fa = q8::factor1(ek[0]), fb = q8::factor1(ek[1]), fa2 = q8::factor2(ek[0]), fb2 = q8::factor2(ek[1]);
+      uint32_t f[2] = {factor_small(ek[0]), factor_small(ek[1])};
+      if (__builtin_expect(two_k, 0)) f[0] = q8::factor1(ek[0]), f[1] = q8::factor1(ek[1]);
 #pragma unroll
       for (int w = 0; w < 8; ++w) {
-        const uint4 ca = xk[0][w >> 2], cb = xk[1][w >> 2];
-        const uint2 a = decode4((w & 3) == 0 ? ca.x : (w & 3) == 1 ? ca.y : (w & 3) == 2 ? ca.z : ca.w, fa, fa2, two);
-        const uint2 d = decode4((w & 3) == 0 ? cb.x : (w & 3) == 1 ? cb.y : (w & 3) == 2 ? cb.z : cb.w, fb, fb2, two);
+        uint2 y[2];
 #pragma unroll
-        for (int n = 0; n < kN; ++n) mma16816(s[n], a.x, d.x, a.y, d.y, q[n][2 * w], q[n][2 * w + 1]);
+        for (int i = 0; i < 2; ++i) {
+          y[i] = spread_pairs(xk[i][w]);
+          y[i].x = q8::mul_bf16x2(y[i].x, f[i]);
+          y[i].y = q8::mul_bf16x2(y[i].y, f[i]);
+          if (__builtin_expect(two_k, 0)) {
+            y[i].x = q8::mul_bf16x2(y[i].x, q8::factor2(ek[i]));
+            y[i].y = q8::mul_bf16x2(y[i].y, q8::factor2(ek[i]));
+          }
+        }
+#pragma unroll
+        for (int n = 0; n < kN; ++n) mma16816(s[n], y[0].x, y[1].x, y[0].y, y[1].y, q[n][2 * w], q[n][2 * w + 1]);
       }
     }
     const int next = step + kFewWarps;
     if (next < hi) load_k(next);
     const int left = keys - step * kFewKeys;   // keys of this step
-    uint32_t pt[kN][2];
+    bool jump = first;
 #pragma unroll
     for (int n = 0; n < kN; ++n) {
       if (g >= left) s[n][0] = s[n][1] = -INFINITY;
       if (g + 8 >= left) s[n][2] = s[n][3] = -INFINITY;
-      float alpha[2];
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        float top = fmaxf(s[n][e], s[n][2 + e]);
+      for (int e = 0; e < 2; ++e) jump = jump || (fmaxf(s[n][e], s[n][2 + e]) - m[n][e]) * p.scale_log2e > kFewJump;
+    }
+    // The reference is the first step's maximum, and moves only where a score is far above it: up to there weights and
+    // sums have the precision that they have near 1.
+    if (__builtin_expect(__any_sync(0xFFFFFFFFu, jump), 0)) {
+      first = false;
 #pragma unroll
-        for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-        // key `step * kFewKeys` is there, so the maximum is one of a score: a first reference, or a larger one
-        const float now = fmaxf(m[n][e], top);
-        alpha[e] = ex2((m[n][e] - now) * p.scale_log2e);
-        m[n][e] = now;
-        const float ref = now * p.scale_log2e;
-        s[n][e] = ex2(fmaf(s[n][e], p.scale_log2e, -ref));
-        s[n][2 + e] = ex2(fmaf(s[n][2 + e], p.scale_log2e, -ref));
-        l[n][e] = fmaf(l[n][e], alpha[e], s[n][e] + s[n][2 + e]);
-      }
-      if (__any_sync(0xFFFFFFFFu, alpha[0] != 1.f || alpha[1] != 1.f)) {
+      for (int n = 0; n < kN; ++n) {
+        float alpha[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float top = fmaxf(s[n][e], s[n][2 + e]);
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+          const float now = fmaxf(m[n][e], top);
+          alpha[e] = ex2((m[n][e] - now) * p.scale_log2e);
+          m[n][e] = now;
+          l[n][e] *= alpha[e];
+        }
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
           o[n][t][0] *= alpha[0];
@@ -180,33 +252,46 @@ window_attn_few_kernel(const __grid_constant__ FewParams p, const uint4* q_rot, 
           o[n][t][3] *= alpha[1];
         }
       }
+    }
+    uint32_t pt[kN][2];
+#pragma unroll
+    for (int n = 0; n < kN; ++n) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float ref = m[n][e] * p.scale_log2e;
+        s[n][e] = ex2(fmaf(s[n][e], p.scale_log2e, -ref));
+        s[n][2 + e] = ex2(fmaf(s[n][2 + e], p.scale_log2e, -ref));
+        l[n][e] += s[n][e] + s[n][2 + e];
+      }
       // P is rounded to bf16, as the operand that the matrix product takes
       pt[n][0] = transpose8x8(pack_bf16x2(s[n][0], s[n][1]));
       pt[n][1] = transpose8x8(pack_bf16x2(s[n][2], s[n][3]));
     }
+    const bool two_v = __any_sync(0xFFFFFFFFu, max(max(ev[0], ev[1]), max(ev[2], ev[3])) > 134u);
     {
-      const bool two = __any_sync(0xFFFFFFFFu, !q8::one_factor(ev[0]) || !q8::one_factor(ev[1]) || !q8::one_factor(ev[2]) ||
-                                                   !q8::one_factor(ev[3]));
-      uint32_t f1[4], f2[4];
+      // factors of the two keys of a pair side by side
+      uint32_t f[2] = {__byte_perm(factor_small(ev[0]), factor_small(ev[1]), 0x5410), __byte_perm(factor_small(ev[2]), factor_small(ev[3]), 0x5410)};
+      if (__builtin_expect(two_v, 0))
+        f[0] = __byte_perm(q8::factor1(ev[0]), q8::factor1(ev[1]), 0x5410), f[1] = __byte_perm(q8::factor1(ev[2]), q8::factor1(ev[3]), 0x5410);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        f1[i] = q8::factor1(ev[i]);
-        f2[i] = q8::factor2(ev[i]);
-      }
+      for (int w = 0; w < 8; ++w) {   // two of the thread's 16 dims
+        uint2 y[2];
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        uint2 y[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          y[i] = decode4(w == 0 ? xv[i].x : w == 1 ? xv[i].y : w == 2 ? xv[i].z : xv[i].w, f1[i], f2[i], two);
-        // dims 4 w .. 4 w + 3 of the two keys of a pair
-#pragma unroll
-        for (int n = 0; n < kN; ++n) {
-          mma16816(o[n][2 * w], __byte_perm(y[0].x, y[1].x, 0x5410), __byte_perm(y[0].x, y[1].x, 0x7632),
-                   __byte_perm(y[2].x, y[3].x, 0x5410), __byte_perm(y[2].x, y[3].x, 0x7632), pt[n][0], pt[n][1]);
-          mma16816(o[n][2 * w + 1], __byte_perm(y[0].y, y[1].y, 0x5410), __byte_perm(y[0].y, y[1].y, 0x7632),
-                   __byte_perm(y[2].y, y[3].y, 0x5410), __byte_perm(y[2].y, y[3].y, 0x7632), pt[n][0], pt[n][1]);
+        for (int i = 0; i < 2; ++i) {
+          const uint4 a = xv[2 * i], d = xv[2 * i + 1];
+          const uint32_t wa = w < 2 ? a.x : w < 4 ? a.y : w < 6 ? a.z : a.w, wd = w < 2 ? d.x : w < 4 ? d.y : w < 6 ? d.z : d.w;
+          // two codes of each key: their pairs are those of a dim
+          y[i] = spread_pairs(__byte_perm(wa, wd, (w & 1) ? 0x7632 : 0x5410));
+          y[i].x = q8::mul_bf16x2(y[i].x, f[i]);
+          y[i].y = q8::mul_bf16x2(y[i].y, f[i]);
+          if (__builtin_expect(two_v, 0)) {
+            const uint32_t f2 = __byte_perm(q8::factor2(ev[2 * i]), q8::factor2(ev[2 * i + 1]), 0x5410);
+            y[i].x = q8::mul_bf16x2(y[i].x, f2);
+            y[i].y = q8::mul_bf16x2(y[i].y, f2);
+          }
         }
+#pragma unroll
+        for (int n = 0; n < kN; ++n) mma16816(o[n][w], y[0].x, y[0].y, y[1].x, y[1].y, pt[n][0], pt[n][1]);
       }
     }
     if (next < hi) load_v(next);
@@ -220,9 +305,9 @@ window_attn_few_kernel(const __grid_constant__ FewParams p, const uint4* q_rot, 
 #pragma unroll
       for (int d = 4; d < 32; d <<= 1) l[n][e] += __shfl_xor_sync(0xFFFFFFFFu, l[n][e], d);
       const int query = 8 * n + 2 * c + e;
-      if (g == 0) warp_ml[warp * 8 * kN + query] = make_float2(m[n][e], l[n][e]);
+      if (g == 0) slab_ml(warp)[query] = make_float2(m[n][e], l[n][e]);
       if (query < p.L) {
-        float* const to = slabs + (warp * 8 * kN + query) * kHeadDim + 16 * g;
+        float* const to = slab(warp, query) + 16 * g;
 #pragma unroll
         for (int t = 0; t < 8; ++t) *reinterpret_cast<float2*>(to + 2 * t) = make_float2(o[n][t][e], o[n][t][2 + e]);
       }
@@ -231,97 +316,149 @@ window_attn_few_kernel(const __grid_constant__ FewParams p, const uint4* q_rot, 
   __syncthreads();
   // weights of parts that saw no key are 0: their reference is -inf, the one of all is not where it counts
   auto weight = [&](float ref, float all) { return ref == -INFINITY ? 0.f : ex2((ref - all) * p.scale_log2e); };
-  for (int i = threadIdx.x; i < p.L * (kHeadDim / 4); i += kFewThreads) {
-    const int query = i / (kHeadDim / 4), col = i - query * (kHeadDim / 4);
-    float all = -INFINITY, sum = 0.f;
-    float2 ml[kFewWarps];
-#pragma unroll
-    for (int w = 0; w < kFewWarps; ++w) {
-      ml[w] = warp_ml[w * 8 * kN + query];
-      all = fmaxf(all, ml[w].x);
-    }
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int w = 0; w < kFewWarps; ++w) {
-      const float f = weight(ml[w].x, all);
-      const float4 x = reinterpret_cast<const float4*>(slabs + (w * 8 * kN + query) * kHeadDim)[col];
-      sum = fmaf(ml[w].y, f, sum);
-      acc.x = fmaf(x.x, f, acc.x);
-      acc.y = fmaf(x.y, f, acc.y);
-      acc.z = fmaf(x.z, f, acc.z);
-      acc.w = fmaf(x.w, f, acc.w);
-    }
-    reinterpret_cast<float4*>(mine)[i] = acc;
-    if (col == 0) my_ml[query] = make_float2(all, sum);
-  }
-  // ---- blocks of the cluster ----
-  __syncthreads();
-  cluster_sync();
-  const uint32_t mine_at = smem_u32(mine), ml_at = smem_u32(my_ml);
-  for (int i = part * kFewThreads + threadIdx.x; i < p.L * (kHeadDim / 4); i += p.parts * kFewThreads) {
-    const int query = i / (kHeadDim / 4), col = i - query * (kHeadDim / 4);
-    float all = -INFINITY, sum = 0.f;
-    float2 ml[kMaxClusterParts];
-#pragma unroll
-    for (int k = 0; k < kMaxClusterParts; ++k) {
-      ml[k] = k < p.parts ? ld_cluster_8(cluster_addr(ml_at + query * 8, k)) : make_float2(-INFINITY, 0.f);
-      all = fmaxf(all, ml[k].x);
-    }
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int k = 0; k < kMaxClusterParts; ++k)
-      if (k < p.parts) {
-        const float f = weight(ml[k].x, all);
-        const float4 x = ld_cluster_16(cluster_addr(mine_at + i * 16, k));
-        sum = fmaf(ml[k].y, f, sum);
-        acc.x = fmaf(x.x, f, acc.x);
-        acc.y = fmaf(x.y, f, acc.y);
-        acc.z = fmaf(x.z, f, acc.z);
-        acc.w = fmaf(x.w, f, acc.w);
-      }
-    const float inv = 1.f / sum;
+  auto add = [](float4& acc, float4 x, float f) {
+    acc.x = fmaf(x.x, f, acc.x);
+    acc.y = fmaf(x.y, f, acc.y);
+    acc.z = fmaf(x.z, f, acc.z);
+    acc.w = fmaf(x.w, f, acc.w);
+  };
+  auto store = [&](int query, int col, float4 acc, float inv) {
     const int64_t dst = (((static_cast<int64_t>(b) * p.L + query) * p.Hn + h) * kHeadDim + 4 * col) / 2;
     UNSTEP_STORE(out, dst, p.extent_out, pack_bf16x2(acc.x * inv, acc.y * inv), p.status);
     UNSTEP_STORE(out, dst + 1, p.extent_out, pack_bf16x2(acc.z * inv, acc.w * inv), p.status);
+  };
+  constexpr int kCols = kHeadDim / 4;
+  float4* const part4 = reinterpret_cast<float4*>(p.part);
+  float2* const part2 = reinterpret_cast<float2*>(p.part);
+  constexpr int kPart4 = few_part_floats<kN>() / 4, kMl2 = 8 * kN * kHeadDim / 2, kPart2 = few_part_floats<kN>() / 2;
+  // the warps' results in shared memory as one, to the scratch or to the result
+  auto merge_warps = [&](bool to_scratch) {
+    for (int i = threadIdx.x; i < p.L * kCols; i += kFewThreads) {
+      const int query = i / kCols, col = i - query * kCols;
+      float all = -INFINITY, sum = 0.f;
+      float2 ml[kFewWarps];
+#pragma unroll
+      for (int w = 0; w < kFewWarps; ++w) {
+        ml[w] = slab_ml(w)[query];
+        all = fmaxf(all, ml[w].x);
+      }
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < kFewWarps; ++w) {
+        const float f = weight(ml[w].x, all);
+        sum = fmaf(ml[w].y, f, sum);
+        add(acc, reinterpret_cast<const float4*>(slab(w, query))[col], f);
+      }
+      if (to_scratch) {
+        UNSTEP_STORE(part4, static_cast<int64_t>(block) * kPart4 + i, p.extent_part / 4, acc, p.status);
+        if (col == 0)
+          UNSTEP_STORE(part2, static_cast<int64_t>(block) * kPart2 + kMl2 + query, p.extent_part / 2, make_float2(all, sum), p.status);
+      } else {
+        store(query, col, acc, 1.f / sum);
+      }
+    }
+  };
+  merge_warps(parts > 1);
+  if (parts == 1) return;
+  // ---- blocks of the item ----
+  const int64_t counter = static_cast<int64_t>(b) * p.Hn + h;
+  __syncthreads();   // all of this part is stored, and shared memory is free
+  if (threadIdx.x == 0) {
+    int before = -1;
+#ifdef UNSTEP_CHECK
+    if (counter >= p.extent_counters) atomicExch(p.status, static_cast<int>(UNSTEP_ERR_BOUNDS));
+    else
+#endif
+    // release: the block's stores (ordered before this thread by the barrier) become visible before the count;
+    // acquire: the last block sees the others' stores
+    asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;" : "=r"(before) : "l"(p.counters + counter) : "memory");
+    last = before == parts - 1;
+    if (last) UNSTEP_STORE(p.counters, counter, p.extent_counters, 0, p.status);   // ready for the next launch
   }
-  __syncwarp();
-  cluster_sync();   // no block leaves while another reads its part
+  __syncthreads();
+  if (!last) return;
+  __threadfence();   // acquire side for every thread that reads the other parts below
+  // every warp merges its share of the parts, a lane four dims, and then the warps merge as above
+  const int64_t part0 = block - part;
+  for (int query = 0; query < p.L; ++query) {
+    float all = -INFINITY, sum = 0.f;
+#pragma unroll 4
+    for (int k = warp; k < parts; k += kFewWarps) all = fmaxf(all, __ldcg(part2 + (part0 + k) * kPart2 + kMl2 + query).x);
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int k = warp; k < parts; k += kFewWarps) {
+      const float2 ml = __ldcg(part2 + (part0 + k) * kPart2 + kMl2 + query);
+      const float f = weight(ml.x, all);
+      sum = fmaf(ml.y, f, sum);
+      add(acc, __ldcg(part4 + (part0 + k) * kPart4 + query * kCols + lane), f);
+    }
+    reinterpret_cast<float4*>(slab(warp, query))[lane] = acc;
+    if (lane == 0) slab_ml(warp)[query] = make_float2(all, sum);
+  }
+  __syncthreads();
+  merge_warps(false);
 }
 
-bool few_setup() {
-  return cudaFuncSetAttribute(window_attn_few_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, few_smem_bytes<1>()) == cudaSuccess &&
-         cudaFuncSetAttribute(window_attn_few_kernel<2>, cudaFuncAttributeMaxDynamicSharedMemorySize, few_smem_bytes<2>()) == cudaSuccess;
+template <int kN>
+static bool few_query(int32_t* blocks) {
+  int n = 0;
+  if (cudaFuncSetAttribute(window_attn_few_kernel<kN>, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewWarps * few_warp_bytes<kN>()) != cudaSuccess ||
+      cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, window_attn_few_kernel<kN>, kFewThreads, kFewWarps * few_warp_bytes<kN>()) != cudaSuccess)
+    return false;
+  *blocks = n;
+  return n > 0;
 }
+bool few_setup(int32_t* blocks_per_sm) { return few_query<1>(blocks_per_sm) && few_query<2>(blocks_per_sm + 1); }
 
-int launch_few(const AttnParams& a, int nb, int sm_count, const void* q_rot, const void* cache_k, const void* scale_k,
-               const void* cache_v, const void* scale_v, void* out, cudaStream_t st) {
+int launch_few(const AttnParams& a, int nb, int sm_count, const int32_t* blocks_per_sm, const void* q_rot, const void* cache_k,
+               const void* scale_k, const void* cache_v, const void* scale_v, void* out, cudaStream_t st) {
+  const bool one = a.L <= 8;
   FewParams p;
   p.Hn = a.Hn;
   p.L = a.L;
+  p.n_streams = nb;
+  p.wide = (reinterpret_cast<uintptr_t>(cache_k) & 31u) == 0;   // heads are 128 bytes
   p.cache_rows = a.cache_rows;
   p.scale_log2e = a.scale_log2e;
-  p.status = status_word();
+  p.part = a.part;
+  p.counters = a.counters;
+  p.status = a.status;
   p.extent_out = static_cast<int64_t>(nb) * a.L * a.Hn * (kHeadDim / 2);
-  int32_t most = 0;
+  p.extent_part = a.extent_part;
+  p.extent_counters = a.extent_counters;
+  int64_t steps[kMaxStreamsPerLaunch], all = 0;
   for (int i = 0; i < nb; ++i) {
     int32_t end = 0;
     for (int r = 0; r < 3; ++r) {
       p.run_row0[i][r] = a.run_row0[i][r];
       p.run_end[i][r] = end += a.run_rows[i][r];
     }
-    most = end > most ? end : most;
+    steps[i] = (end + kFewKeys - 1) / kFewKeys;
+    all += steps[i] * a.Hn;
   }
-  // blocks for two on each SM, but none with less than a step for every warp
-  const int64_t items = static_cast<int64_t>(nb) * a.Hn;
-  int64_t parts = (2 * sm_count + items - 1) / items;
-  const int64_t fill = (most + kFewKeys * kFewWarps - 1) / (kFewKeys * kFewWarps);
-  if (parts > fill) parts = fill;
-  if (parts > kMaxClusterParts) parts = kMaxClusterParts;
-  p.parts = static_cast<int32_t>(parts);
-  const bool one = a.L <= 8;
-  const cudaError_t err = launch_clusters(
-      true, p.parts, one ? window_attn_few_kernel<1> : window_attn_few_kernel<2>, dim3(static_cast<unsigned>(items * parts)),
-      kFewThreads, one ? few_smem_bytes<1>() : few_smem_bytes<2>(), st, p, static_cast<const uint4*>(q_rot),
+  // The shortest share of steps for a block with which all blocks run at once (a second wave would take as long as
+  // the first), but at least one for each of its warps; with more items than blocks an item is not split.
+  const int64_t room = static_cast<int64_t>(sm_count) * blocks_per_sm[one ? 0 : 1];
+  const int64_t part_room = p.extent_part / (one ? few_part_floats<1>() : few_part_floats<2>());
+  int64_t share = (all + room - 1) / room, blocks = 0;
+  if (share < kFewWarps) share = kFewWarps;
+  for (int i = 0; i < nb; ++i)   // and no more than kFewParts blocks, which one of them merges
+    if (share < (steps[i] + kFewParts - 1) / kFewParts) share = (steps[i] + kFewParts - 1) / kFewParts;
+  for (;; share += share / 16 + 1) {
+    blocks = 0;
+    bool split = false;
+    for (int i = 0; i < nb; ++i) {
+      const int64_t parts = (steps[i] + share - 1) / share;
+      p.parts[i] = static_cast<int32_t>(parts);
+      p.block0[i] = static_cast<int32_t>(blocks);
+      blocks += parts * a.Hn;
+      split = split || parts > 1;
+    }
+    if (!split || (blocks <= room && blocks <= part_room)) break;
+  }
+  const cudaError_t err = launch_overlapped(
+      true, one ? window_attn_few_kernel<1> : window_attn_few_kernel<2>, dim3(static_cast<unsigned>(blocks)), kFewThreads,
+      one ? kFewWarps * few_warp_bytes<1>() : kFewWarps * few_warp_bytes<2>(), st, p, static_cast<const uint4*>(q_rot),
       static_cast<const uint4*>(cache_k), static_cast<const uint8_t*>(scale_k), static_cast<const uint4*>(cache_v),
       static_cast<const uint8_t*>(scale_v), static_cast<uint32_t*>(out));
   g_launches.fetch_add(1);

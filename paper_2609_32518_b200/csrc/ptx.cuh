@@ -257,6 +257,12 @@ __device__ __forceinline__ void st_global_32(void* p, const uint32_t* r) {
                "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                : "memory");
 }
+// One 32-byte load (the address must be 32-byte aligned).
+__device__ __forceinline__ void ld_global_32(const void* p, uint32_t* r) {
+  asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "l"(p) : "memory");
+}
 // ------------------------------------------------- clusters: each other's shared memory
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
