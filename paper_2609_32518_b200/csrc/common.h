@@ -139,6 +139,18 @@ __device__ __forceinline__ int grid_wait() {
 // needs a whole SM, which it only gets when their blocks there are done.  The attention does not:
 // blocks of the next kernel that wait on SMs it leaves idle would keep other streams' work from them.
 __device__ __forceinline__ void grid_launch_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+// A block that is set up while the kernel before it finishes has DRAM bring its inputs to L2 meanwhile.
+// The prefetch reads nothing: L2 is where that kernel's stores become visible, and the loads behind
+// grid_wait() find whatever is there by then.  Only the blocks that fit the GPU at once can be early,
+// and only launches of up to 64 MB of inputs ask for it: the append behind the norm of 4680 tokens x 12
+// heads (43 MB of inputs) 17.8 -> 16.6 us, the plain one in front of 4680 keys' attention 157.4 -> 156.9
+// with it; four streams (172 MB) 55.5 -> 55.8, so that they do without.
+constexpr int64_t kPrefetchVectors = (int64_t{64} << 20) / 16;
+constexpr int kEarlyBlocks = 2048;
+__device__ __forceinline__ void prefetch_l2(const uint4* p, int vectors) {
+  asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(vectors * 16) : "memory");
+}
 #endif
 
 // The device the call will run on must be sm_100.

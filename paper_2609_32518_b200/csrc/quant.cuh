@@ -5,6 +5,8 @@
 #include <cuda_bf16.h>
 #include <stdint.h>
 
+#include "ptx.cuh"
+
 namespace unstep {
 namespace q8 {
 
@@ -28,20 +30,35 @@ __device__ __forceinline__ uint32_t cvt_e4m3x2(float lo, float hi) {
   return r;
 }
 
+// Larger of magnitudes, a NaN if one of them is: its bits are then above kTooLarge.
+__device__ __forceinline__ float max_abs(float a, float b) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(fabsf(a)), "f"(fabsf(b)));
+  return d;
+}
+__device__ __forceinline__ float max_abs(float a, float b, float c) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(fabsf(a)), "f"(fabsf(b)), "f"(fabsf(c)));
+  return d;
+}
+
 // Quantises 8 values of a thread; the four threads of a block of 32 are neighbouring lanes that all come here.
 __device__ __forceinline__ uint2 quantise8(const float* y, uint32_t* byte) {
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(y[i]) & 0x7FFFFFFFu);
-  top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-  top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-  const uint32_t e = scale_byte(top);
+  float top = max_abs(max_abs(max_abs(y[0], y[1], y[2]), y[3], y[4]), max_abs(y[5], y[6], y[7]));
+  top = max_abs(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+  top = max_abs(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+  const uint32_t e = scale_byte(__float_as_uint(top));
   *byte = e;
   if (e == kNanByte) return make_uint2(0u, 0u);
   const float inverse = __uint_as_float((254u - e) << 23);   // 2^(127 - e), a product with it is exact
+  const uint64_t inverse2 = ptx::pack_f32x2(inverse, inverse);
   uint32_t c[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) c[i] = cvt_e4m3x2(y[2 * i] * inverse, y[2 * i + 1] * inverse);
+  for (int i = 0; i < 4; ++i) {
+    float lo, hi;
+    ptx::unpack_f32x2(ptx::mul_f32x2(ptx::pack_f32x2(y[2 * i], y[2 * i + 1]), inverse2), lo, hi);
+    c[i] = cvt_e4m3x2(lo, hi);
+  }
   return make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
 }
 

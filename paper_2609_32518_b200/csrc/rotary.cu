@@ -22,16 +22,17 @@ template <bool kHalf>
 struct Coefficients {
   float c[kHalf ? 8 : 4], s[kHalf ? 8 : 4];
 };
-template <bool kHalf>
-__device__ __forceinline__ Coefficients<kHalf> load_coefficients(const RotaryPlace& p, const float4* cos_t, const float4* sin_t,
-                                                                 int64_t row, int u) {
+// `load(i)`: cosines and sines of quad i of the table's row.
+template <bool kHalf, typename Load>
+__device__ __forceinline__ Coefficients<kHalf> coefficients(const RotaryPlace& p, int u, const Load& load) {
   Coefficients<kHalf> k;
   constexpr int kQuads = kHalf ? 2 : 1;
   const bool second = kHalf && u >= p.shift;
-  const int64_t at = row + (kHalf ? 2 * (second ? u - p.shift : u) : u);
+  const int at = kHalf ? 2 * (second ? u - p.shift : u) : u;
 #pragma unroll
   for (int i = 0; i < kQuads; ++i) {
-    const float4 c = __ldca(cos_t + at + i), s = __ldca(sin_t + at + i);
+    float4 c, s;
+    load(at + i, c, s);
     k.c[4 * i] = c.x, k.c[4 * i + 1] = c.y, k.c[4 * i + 2] = c.z, k.c[4 * i + 3] = c.w;
     k.s[4 * i] = s.x, k.s[4 * i + 1] = s.y, k.s[4 * i + 2] = s.z, k.s[4 * i + 3] = s.w;
   }
@@ -39,6 +40,14 @@ __device__ __forceinline__ Coefficients<kHalf> load_coefficients(const RotaryPla
 #pragma unroll
   for (int i = 0; i < 4 * kQuads; ++i) k.s[i] = __uint_as_float(__float_as_uint(k.s[i]) ^ flip);
   return k;
+}
+template <bool kHalf>
+__device__ __forceinline__ Coefficients<kHalf> load_coefficients(const RotaryPlace& p, const float4* cos_t, const float4* sin_t,
+                                                                 int64_t row, int u) {
+  return coefficients<kHalf>(p, u, [&](int i, float4& c, float4& s) {
+    c = __ldca(cos_t + row + i);
+    s = __ldca(sin_t + row + i);
+  });
 }
 
 __device__ __forceinline__ void unpack8(uint4 x, float* f) {
@@ -66,9 +75,18 @@ __device__ __forceinline__ void rotate_pairs(const float* x, const Coefficients<
     y[2 * i + 1] = __fadd_rn(__fmul_rn(x[2 * i], k.s[i]), __fmul_rn(x[2 * i + 1], k.c[i]));
   }
 }
+// (Products two at a time.  Sums are not: a packed product and a packed sum are contracted to one rounding, .rn or not.)
 __device__ __forceinline__ void rotate_halves(const float* x, const float* other, const Coefficients<true>& k, float* y) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) y[i] = __fadd_rn(__fmul_rn(x[i], k.c[i]), __fmul_rn(other[i], k.s[i]));
+  for (int i = 0; i < 8; i += 2) {
+    const uint64_t a = ptx::mul_f32x2(ptx::pack_f32x2(x[i], x[i + 1]), ptx::pack_f32x2(k.c[i], k.c[i + 1]));
+    const uint64_t b = ptx::mul_f32x2(ptx::pack_f32x2(other[i], other[i + 1]), ptx::pack_f32x2(k.s[i], k.s[i + 1]));
+    float a0, a1, b0, b1;
+    ptx::unpack_f32x2(a, a0, a1);
+    ptx::unpack_f32x2(b, b0, b1);
+    y[i] = __fadd_rn(a0, b0);
+    y[i + 1] = __fadd_rn(a1, b1);
+  }
 }
 __device__ __forceinline__ uint4 shuffle16(uint4 x, int from) {
   return make_uint4(__shfl_sync(0xFFFFFFFFu, x.x, from), __shfl_sync(0xFFFFFFFFu, x.y, from),
@@ -133,18 +151,19 @@ rotary_apply_kernel(const ApplyParams p, const uint4* x_in, const float4* cos_t,
 }
 
 // --------------------------------------------------------------------------
-// Append into the 8-bit cache.  A thread has the same place of kU heads of a token in q, k and v, `width` vectors
-// apart; without the norm the threads of all tokens are one sequence, with it a block has a token (kWide: more
-// vectors than its threads hold, read a second time behind the sum of squares).  Four neighbouring threads
-// hold a block of 32 dims and find its largest magnitude with two shuffles.
+// Append into the 8-bit cache.  `width` threads have a token: a thread the same place of kU heads in q, k and v, `width`
+// vectors apart (kWide: more than that, kU at a time); a block has one token with the norm, whose sum meets in shared memory, else
+// `tokens` of them.  Four neighbouring threads hold a block of 32 dims and find its largest magnitude with two shuffles.
 // --------------------------------------------------------------------------
 struct Append8Params {
   RotaryPlace place;
-  int32_t L, T, C, S, vec_per_token, width;
+  int32_t L, T, C, S, vec_per_token, width, tokens;
+  int32_t frame0;                  // with the norm: first frame of this launch inside the chunk
   int64_t vec_per_stream;          // L * Hn * 16
   int64_t cache_vec_per_stream;    // (S + C) * T * Hn * 16 vectors of 8 codes
-  float eps;
+  float eps, channels;             // channels: Hn * 128
   int32_t start[kMaxStreamsPerLaunch];
+  int32_t prefetch;                // 1: the first blocks prefetch their inputs to L2
   int* status;                     // extents of q_out (16-byte vectors), codes (8-byte vectors) and scale bytes
   int64_t extent_act, extent_code, extent_scale;
 };
@@ -154,47 +173,60 @@ __device__ __forceinline__ float warp_sum32(float x) {
   for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
   return x;
 }
-__device__ __forceinline__ float squares32(uint4 x, float acc) {
+// Sum of the squares of a vector, added to the two halves of `acc`.
+__device__ __forceinline__ uint64_t squares32(uint4 x, uint64_t acc) {
   float f[8];
   unpack8(x, f);
-  float s0 = 0.f, s1 = 0.f;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    s0 = fmaf(f[2 * i], f[2 * i], s0);
-    s1 = fmaf(f[2 * i + 1], f[2 * i + 1], s1);
+  for (int i = 0; i < 8; i += 2) {
+    const uint64_t v = ptx::pack_f32x2(f[i], f[i + 1]);
+    acc = ptx::fma_f32x2(v, v, acc);
   }
-  return acc + (s0 + s1);
+  return acc;
 }
+// f * r * gain, each product rounded to float32
 __device__ __forceinline__ void gain8(float* f, float r, const float4* gain, int vi) {
   const float4 g0 = __ldca(gain + 2 * vi), g1 = __ldca(gain + 2 * vi + 1);
   const float g[8] = {g0.x, g0.y, g0.z, g0.w, g1.x, g1.y, g1.z, g1.w};
+  const uint64_t r2 = ptx::pack_f32x2(r, r);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) f[i] = __fmul_rn(__fmul_rn(f[i], r), g[i]);
+  for (int i = 0; i < 8; i += 2)
+    ptx::unpack_f32x2(ptx::mul_f32x2(ptx::mul_f32x2(ptx::pack_f32x2(f[i], f[i + 1]), r2), ptx::pack_f32x2(g[i], g[i + 1])), f[i], f[i + 1]);
 }
 
 template <int kU, bool kHalf, bool kNorm, bool kWide>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(kNorm && kU <= 2 ? 96 : 256, kNorm && kU <= 2 ? 10 : 1)
 rotary_kv_append_q8_kernel(const Append8Params p, const uint4* q_in, const uint4* k_in, const uint4* v_in,
                            const float4* gain_q, const float4* gain_k, const float4* cos_t, const float4* sin_t,
                            uint4* q_out, uint2* cache_k, uint8_t* scale_k, uint2* cache_v, uint8_t* scale_v) {
   __shared__ float part[2][8];
+  __shared__ float4 table[2][16];   // with the norm: the token's row, which is used behind the sum
   grid_launch_next();
-  const int b = blockIdx.y;
-  int n, i0;
+  const int b = blockIdx.z;
+  int n, f, t, i0 = threadIdx.x;
+  bool live = true;
   if (kNorm) {
-    n = blockIdx.x;
-    i0 = threadIdx.x;
+    t = blockIdx.x;
+    f = p.frame0 + blockIdx.y;
+    n = f * p.T + t;
   } else {
-    const int64_t id = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
-    n = static_cast<int>(id / p.width);
-    i0 = static_cast<int>(id - static_cast<int64_t>(n) * p.width);
+    const int token = i0 / p.width;   // one more than there are where the block is filled up to whole warps
+    n = blockIdx.x * p.tokens + token;
+    i0 -= token * p.width;
+    live = token < p.tokens && n < p.L;
+    f = n / p.T;
+    t = n - f * p.T;
   }
-  const bool live = n < p.L;
-  const int f = n / p.T, t = n - f * p.T;
   const int frame = p.start[b] + f;
   const int slot = frame < p.S ? frame : p.S + (frame - p.S) % p.C;
   const int u = i0 & 15;
   const bool rotated = u < p.place.rows;
+  if (kNorm && p.prefetch && threadIdx.x == 0 && (blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x < kEarlyBlocks) {
+    const int64_t first = static_cast<int64_t>(b) * p.vec_per_stream + static_cast<int64_t>(n) * p.vec_per_token;
+    prefetch_l2(q_in + first, p.vec_per_token);
+    prefetch_l2(k_in + first, p.vec_per_token);
+    prefetch_l2(v_in + first, p.vec_per_token);
+  }
   const int behind = grid_wait();
   i0 += behind;   // every load below goes by i0
   const int64_t in_base = static_cast<int64_t>(b) * p.vec_per_stream + static_cast<int64_t>(n) * p.vec_per_token;
@@ -215,39 +247,66 @@ rotary_kv_append_q8_kernel(const Append8Params p, const uint4* q_in, const uint4
       xv[j] = mine ? __ldcs(v_in + in_base + i) : zero;
     }
   };
+  auto put = [&](const float* y, int i, uint2* cache, uint8_t* scale) {
+    uint32_t byte;
+    const uint2 codes = q8::quantise8(y, &byte);
+    if (live && i < p.vec_per_token) {
+      const int64_t dst = cache_base + i;
+      UNSTEP_STORE(cache, dst, p.extent_code, codes, p.status);
+      // a word of the head's four bytes from one lane costs two more shuffles: 62 instead of 58 us for four streams
+      if ((u & 3) == 0) UNSTEP_STORE(scale, dst >> 2, p.extent_scale, static_cast<uint8_t>(byte), p.status);
+    }
+  };
   float rq = 1.f, rk = 1.f;
   load(i0);
   Coefficients<kHalf> k = {};
-  if (live && rotated)
-    k = load_coefficients<kHalf>(p.place, cos_t, sin_t, b * p.place.stride4 + static_cast<int64_t>(n) * p.place.rows + behind, u);
+  const int64_t table_row = b * p.place.stride4 + static_cast<int64_t>(n) * p.place.rows + behind;
   if (kNorm) {
-    float sq = 0.f, sk = 0.f;
+    if (threadIdx.x < 32 && u < p.place.rows) table[threadIdx.x >> 4][u] = __ldca((threadIdx.x < 16 ? cos_t : sin_t) + table_row + u);
+    // v does without the sum, and its registers are free behind this
+    if (!kWide) {
+#pragma unroll
+      for (int j = 0; j < kU; ++j) {
+        float y[8];
+        unpack8(xv[j], y);
+        put(y, i0 + j * p.width, cache_v, scale_v);
+      }
+    }
+    uint64_t sq2 = 0, sk2 = 0;
     for (int at = i0;;) {
 #pragma unroll
       for (int j = 0; j < kU; ++j) {
-        sq = squares32(xq[j], sq);
-        sk = squares32(xk[j], sk);
+        sq2 = squares32(xq[j], sq2);
+        sk2 = squares32(xk[j], sk2);
       }
       at += step;
       if (!kWide || at - i0 >= p.vec_per_token) break;
       load(at);
     }
-    sq = warp_sum32(sq);
-    sk = warp_sum32(sk);
+    float a, d;
+    ptx::unpack_f32x2(sq2, a, d);
+    const float sq = warp_sum32(a + d);
+    ptx::unpack_f32x2(sk2, a, d);
+    const float sk = warp_sum32(a + d);
     if ((threadIdx.x & 31) == 0) {
       part[0][threadIdx.x >> 5] = sq;
       part[1][threadIdx.x >> 5] = sk;
     }
     __syncthreads();
-    sq = sk = 0.f;
-    for (int w = 0; w < static_cast<int>(blockDim.x >> 5); ++w) {
-      sq += part[0][w];
-      sk += part[1][w];
-    }
-    const float width = static_cast<float>(p.vec_per_token) * 8.f;
-    rq = __frcp_rn(__fsqrt_rn(__fadd_rn(__fdiv_rn(sq, width), p.eps)));
-    rk = __frcp_rn(__fsqrt_rn(__fadd_rn(__fdiv_rn(sk, width), p.eps)));
+    // even lanes finish q, odd lanes k: one division and one root per warp
+    float sum = 0.f;
+    for (int w = 0; w < static_cast<int>(blockDim.x >> 5); ++w) sum += part[threadIdx.x & 1][w];
+    const float r = __frcp_rn(__fsqrt_rn(__fadd_rn(__fdiv_rn(sum, p.channels), p.eps)));
+    rq = __shfl_sync(0xFFFFFFFFu, r, 0);
+    rk = __shfl_sync(0xFFFFFFFFu, r, 1);
     if (kWide) load(i0);
+    if (rotated)
+      k = coefficients<kHalf>(p.place, u, [&](int i, float4& c, float4& s) {
+        c = table[0][i];
+        s = table[1][i];
+      });
+  } else if (live && rotated) {
+    k = load_coefficients<kHalf>(p.place, cos_t, sin_t, table_row, u);
   }
   // float32 values behind the norm and the rotation
   auto turn = [&](uint4 x, float r, const float4* gain, int vi, float* y) {
@@ -275,23 +334,14 @@ rotary_kv_append_q8_kernel(const Append8Params p, const uint4* q_in, const uint4
 #pragma unroll
     for (int j = 0; j < kU; ++j) {
       const int i = at + j * p.width;
-      const bool mine = live && i < p.vec_per_token;
       float y[8];
       turn(xq[j], rq, gain_q, i, y);
-      if (mine) UNSTEP_STORE(q_out, in_base + i, p.extent_act, pack8(y), p.status);
-      uint32_t byte_k, byte_v;
+      if (live && i < p.vec_per_token) UNSTEP_STORE(q_out, in_base + i, p.extent_act, pack8(y), p.status);
       turn(xk[j], rk, gain_k, i, y);
-      const uint2 ck = q8::quantise8(y, &byte_k);
-      unpack8(xv[j], y);
-      const uint2 cv = q8::quantise8(y, &byte_v);
-      if (mine) {
-        const int64_t dst = cache_base + i;
-        UNSTEP_STORE(cache_k, dst, p.extent_code, ck, p.status);
-        UNSTEP_STORE(cache_v, dst, p.extent_code, cv, p.status);
-        if ((u & 3) == 0) {
-          UNSTEP_STORE(scale_k, dst >> 2, p.extent_scale, static_cast<uint8_t>(byte_k), p.status);
-          UNSTEP_STORE(scale_v, dst >> 2, p.extent_scale, static_cast<uint8_t>(byte_v), p.status);
-        }
+      put(y, i, cache_k, scale_k);
+      if (!kNorm || kWide) {
+        unpack8(xv[j], y);
+        put(y, i, cache_v, scale_v);
       }
     }
     at += step;
@@ -402,7 +452,15 @@ typedef void (*Append8Kernel)(const Append8Params, const uint4*, const uint4*, c
                               const float4*, const float4*, uint4*, uint2*, uint8_t*, uint2*, uint8_t*);
 template <bool kHalf>
 static Append8Kernel append8_kernel(bool norm, int per_thread, bool wide) {
-  if (!norm) return per_thread == 1 ? rotary_kv_append_q8_kernel<1, kHalf, false, false> : rotary_kv_append_q8_kernel<2, kHalf, false, false>;
+  if (!norm) {
+    if (wide) return rotary_kv_append_q8_kernel<4, kHalf, false, true>;
+    switch (per_thread) {
+      case 1: return rotary_kv_append_q8_kernel<1, kHalf, false, false>;
+      case 2: return rotary_kv_append_q8_kernel<2, kHalf, false, false>;
+      case 3: return rotary_kv_append_q8_kernel<3, kHalf, false, false>;
+      default: return rotary_kv_append_q8_kernel<4, kHalf, false, false>;
+    }
+  }
   if (wide) return rotary_kv_append_q8_kernel<4, kHalf, true, true>;
   switch (per_thread) {
     case 1: return rotary_kv_append_q8_kernel<1, kHalf, true, false>;
@@ -448,6 +506,7 @@ extern "C" int unstep_rotary_kv_append_q8(const unstep_shape_t* shape, const uns
   p.vec_per_stream = L * p.vec_per_token;
   p.cache_vec_per_stream = (static_cast<int64_t>(shape->ring_frames) + sink_frames) * T * p.vec_per_token;
   p.eps = eps;
+  p.channels = static_cast<float>(shape->heads * kHeadDim);
   p.status = status_word();
   int threads = 256, per_thread = 1;
   bool wide = false;
@@ -459,11 +518,19 @@ extern "C" int unstep_rotary_kv_append_q8(const unstep_shape_t* shape, const uns
     wide = threads > 256;
     if (wide) threads = 256;
     p.width = threads;
-    blocks = L;
+    p.tokens = 1;
+    blocks = T;
   } else {
-    per_thread = shape->heads > 1 ? 2 : 1;
-    p.width = 16 * ((shape->heads + per_thread - 1) / per_thread);
-    blocks = (L * p.width + 255) / 256;
+    // three heads a thread, or the number of heads that leaves fewer of them without work
+    wide = shape->heads > 64;
+    per_thread = 3;
+    for (const int u : {4, 2, 1})
+      if ((shape->heads + u - 1) / u * u < (shape->heads + per_thread - 1) / per_thread * per_thread) per_thread = u;
+    if (wide || shape->heads > 16 * per_thread) per_thread = 4;
+    p.width = wide ? 256 : 16 * ((shape->heads + per_thread - 1) / per_thread);
+    p.tokens = 256 / p.width;
+    threads = (p.width * p.tokens + 31) & ~31;
+    blocks = (L + p.tokens - 1) / p.tokens;
   }
   if (blocks > INT32_MAX) return UNSTEP_ERR_INVALID_ARG;
   const Append8Kernel kernel = rope->half ? append8_kernel<true>(norm, per_thread, wide) : append8_kernel<false>(norm, per_thread, wide);
@@ -471,18 +538,25 @@ extern "C" int unstep_rotary_kv_append_q8(const unstep_shape_t* shape, const uns
     const int nb = shape->batch - b0 < kMaxStreamsPerLaunch ? shape->batch - b0 : kMaxStreamsPerLaunch;
     for (int i = 0; i < nb; ++i) p.start[i] = start_frame[b0 + i];
     p.extent_act = nb * p.vec_per_stream;
+    p.prefetch = 3 * p.extent_act <= kPrefetchVectors;
     p.extent_code = nb * p.cache_vec_per_stream;
     p.extent_scale = p.extent_code / 4;
     const int64_t in = b0 * p.vec_per_stream, cache = b0 * p.cache_vec_per_stream, tab = b0 * table_stream_stride;
-    const cudaError_t err = launch_overlapped(
-        true, kernel, dim3(static_cast<unsigned>(blocks), nb), threads, 0, static_cast<cudaStream_t>(cuda_stream), p,
-        static_cast<const uint4*>(q_in) + in, static_cast<const uint4*>(k_in) + in, static_cast<const uint4*>(v_in) + in,
-        reinterpret_cast<const float4*>(gain_q), reinterpret_cast<const float4*>(gain_k),
-        reinterpret_cast<const float4*>(cos + tab), reinterpret_cast<const float4*>(sin + tab), static_cast<uint4*>(q_out) + in,
-        static_cast<uint2*>(cache_k) + cache, static_cast<uint8_t*>(scale_k) + cache / 4, static_cast<uint2*>(cache_v) + cache,
-        static_cast<uint8_t*>(scale_v) + cache / 4);
-    g_launches.fetch_add(1);
-    if (err != cudaSuccess) return UNSTEP_ERR_CUDA;
+    constexpr int kMaxFrames = 65535;
+    for (p.frame0 = 0; p.frame0 < shape->chunk_frames; p.frame0 += kMaxFrames) {
+      const int left = shape->chunk_frames - p.frame0;
+      const int frames = norm ? (left < kMaxFrames ? left : kMaxFrames) : 1;
+      const cudaError_t err = launch_overlapped(
+          true, kernel, dim3(static_cast<unsigned>(blocks), frames, nb), threads, 0, static_cast<cudaStream_t>(cuda_stream), p,
+          static_cast<const uint4*>(q_in) + in, static_cast<const uint4*>(k_in) + in, static_cast<const uint4*>(v_in) + in,
+          reinterpret_cast<const float4*>(gain_q), reinterpret_cast<const float4*>(gain_k),
+          reinterpret_cast<const float4*>(cos + tab), reinterpret_cast<const float4*>(sin + tab), static_cast<uint4*>(q_out) + in,
+          static_cast<uint2*>(cache_k) + cache, static_cast<uint8_t*>(scale_k) + cache / 4, static_cast<uint2*>(cache_v) + cache,
+          static_cast<uint8_t*>(scale_v) + cache / 4);
+      g_launches.fetch_add(1);
+      if (err != cudaSuccess) return UNSTEP_ERR_CUDA;
+      if (!norm || left <= kMaxFrames) break;
+    }
   }
   return UNSTEP_OK;
 }
