@@ -80,7 +80,14 @@ constexpr int kHalfBytes = 128 * 64 * 2;    // one TMA box: 128 rows x 64 bf16 (
 constexpr int kTileBytes = 2 * kHalfBytes;  // 128 x 128 bf16
 // What the kernel over a bf16 cache and the one over an 8-bit cache have of their own.  The latter has four more
 // warps, which decode the tiles that TMA brings as codes (kRawStages buffers) into the bf16 buffers that the other has TMA fill.
+//
+// Where every item has one query tile (kQ8Lone), the second softmax group has nothing to do and the second Q buffer is free: the
+// group then decodes the V tiles and the four warps the K tiles, and K and V have a ring each, of two tiles as codes and
+// two as bf16.  (Rings that both kinds go through in turn do not do for that: a warp has to see every phase of a barrier
+// that it waits at, as it cannot tell one from the phase before the last.)
 constexpr int kRawStages = 2, kRawBytes = 128 * 128;
+enum Kind { kBf16, kQ8Pairs, kQ8Lone };
+constexpr int kKinds = 3;
 template <bool kQ8>
 struct Form {
   static constexpr int kStages = kQ8 ? 4 : 5;       // 32 KB buffers shared by the K and V tiles
@@ -361,14 +368,15 @@ __device__ __forceinline__ void decode_row(uint32_t src, uint32_t dst, uint32_t 
 // kCluster: a launch of one part per block, in which the parts of an item are a cluster and merge through each
 // other's shared memory.  The other form merges through global memory, where a part's stores, the fence
 // with its count and the last part's loads took 5-10 us one after the other.
-// kQ8: over an 8-bit cache.  tm_kf and tm_vf are maps over codes then, and tm_k and tm_v are not used: the decoders write
+// kKind: kBf16, or over an 8-bit cache (kQ8).  Then tm_kf and tm_vf are maps over codes, and tm_k and tm_v are not used: the decoders write
 // all rows of a tile, so that a ragged one needs no zero fill, and frames of any length lie in runs of keys.
-template <bool kCluster, bool kQ8>
-__global__ void __launch_bounds__(Form<kQ8>::kThreads, 1)
+template <bool kCluster, Kind kKind>
+__global__ void __launch_bounds__(Form<kKind != kBf16>::kThreads, 1)
 window_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                    const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_kf,
                    const __grid_constant__ CUtensorMap tm_vf, const AttnParams p,
                    __nv_bfloat16* __restrict__ out) {
+  constexpr bool kQ8 = kKind != kBf16, lone = kKind == kQ8Lone;
   constexpr int kStages = Form<kQ8>::kStages;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   const uint32_t smem_base = smem_u32(smem_raw);
@@ -387,8 +395,8 @@ window_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   const uint32_t bar_kv_empty = sBar + 32 + 8 * kStages;     // [kStages] that issuer -> TMA
   const uint32_t bar_s_full = sBar + 32 + 16 * kStages;      // [2]  Q K^T issuer -> softmax a
   const uint32_t bar_pv_done = bar_s_full + 16;              // [2]  P V issuer -> softmax a
-  const uint32_t bar_raw_full = bar_pv_done + 16;            // kQ8: [kRawStages] TMA -> decoders
-  const uint32_t bar_raw_empty = bar_raw_full + 8 * kRawStages;   // kQ8: [kRawStages] decoders -> TMA
+  const uint32_t bar_raw_full = bar_pv_done + 16;            // kQ8: [2 kRawStages] TMA -> decoders
+  const uint32_t bar_raw_empty = bar_raw_full + 16 * kRawStages;  // kQ8: [2 kRawStages] decoders -> TMA
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen + kSmemBar + 224);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(gen + kSmemBar + 228);
 
@@ -408,7 +416,7 @@ window_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       mbar_init(bar_kv_full + 8 * i, kQ8 ? 4 : 1);
       mbar_init(bar_kv_empty + 8 * i, 1);
     }
-    for (int i = 0; kQ8 && i < kRawStages; ++i) {
+    for (int i = 0; kQ8 && i < 2 * kRawStages; ++i) {
       mbar_init(bar_raw_full + 8 * i, 1);
       mbar_init(bar_raw_empty + 8 * i, 4);
     }
@@ -427,35 +435,44 @@ window_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   // there, so that no bounded wait counts that kernel's time.
   const Waiter w{abort_flag, kWaitCycles};
 
-  if (kQ8 && warp >= 12) {
-    // ---------------------------------------------------------------- decoders
-    // A thread has a row (key) of every tile.  Its scale word comes straight from global memory, a tile ahead.
-    reg_dealloc_decode();
-    grid_wait();
+  // Buffer and phase of a tile that is the `it`-th of all and the `c`-th of its kind.
+  auto kv_stage = [&](bool is_v, uint32_t it, uint32_t c) { return lone ? 2 * is_v + (c & 1) : it % kStages; };
+  auto kv_phase = [&](uint32_t it, uint32_t c) { return lone ? c >> 1 : it / kStages; };
+  auto raw_stage = [&](bool is_v, uint32_t it, uint32_t c) { return lone ? kRawStages * is_v + (c & 1) : it % kRawStages; };
+  auto raw_phase = [&](uint32_t it, uint32_t c) { return lone ? c >> 1 : it / kRawStages; };
+  auto raw_buffer = [&](uint32_t stage) {
+    return smem_base + (stage < kRawStages ? kSmemRaw + stage * kRawBytes : kSmemQ + kTileBytes + (stage - kRawStages) * kRawBytes);
+  };
+  // kQ8, a decoding warp: thread `row` has that row (key) of every tile, lone: of every K tile or every V tile.  Its scale word
+  // comes straight from global memory, a tile ahead.
+  auto decode_tiles = [&](const int row, const bool values) {
     Sched sched(p, static_cast<int>(blockIdx.x));
     Seg s;
-    const int row = tid - 384;
     const uint32_t swizzle = row & 7;
-    uint32_t it = 0;
+    uint32_t c0 = 0;   // tiles of a kind before this segment
     bool ok = true;
     while (ok && sched.next(s)) {
-      const int n = 2 * (s.t1 - s.t0);
-      auto word_of = [&](int i) {   // the i-th of the item's K and V tiles, in the order in which they come
-        const bool is_v = i > 0 && ((i & 1) == 0 || i == n - 1);
-        const TileInfo ti = tile_info(p, s.b, s.t0 + (i == n - 1 ? n / 2 - 1 : is_v ? i / 2 - 1 : (i + 1) / 2));
+      const int tiles = s.t1 - s.t0, n = lone ? tiles : 2 * tiles;
+      // The i-th tile: lone, of its kind; else they come as K of the first, then K and V in turn, V of the last.
+      auto is_value = [&](int i) { return lone ? values : i > 0 && ((i & 1) == 0 || i == n - 1); };
+      auto index = [&](int i) { return lone ? i : i == n - 1 ? tiles - 1 : is_value(i) ? i / 2 - 1 : (i + 1) / 2; };
+      auto word_of = [&](int i) {
+        const TileInfo ti = tile_info(p, s.b, s.t0 + index(i));
         if (row >= ti.valid) return 0u;   // nobody attends it: any finite value will do
-        return ld_global_4((is_v ? p.scale_v : p.scale_k) + (s.b * p.cache_rows + ti.row + row) * p.Hn + s.h);
+        return ld_global_4((is_value(i) ? p.scale_v : p.scale_k) + (s.b * p.cache_rows + ti.row + row) * p.Hn + s.h);
       };
       uint32_t ahead = word_of(0);
 #pragma unroll 1
-      for (int i = 0; i < n; ++i, ++it) {
+      for (int i = 0; i < n; ++i) {
         const uint32_t word = ahead;
         if (i + 1 < n) ahead = word_of(i + 1);
-        const uint32_t raw = it % kRawStages, st = it % kStages;
-        ok = w.wait_warp(bar_raw_full + 8 * raw, (it / kRawStages) & 1);
-        if (ok) ok = w.wait_warp(bar_kv_empty + 8 * st, ((it / kStages) & 1) ^ 1);
+        const uint32_t it = 2 * c0 + i, c = c0 + i;   // lone or not, only one of them is looked at
+        const bool is_v = lone && values;
+        const uint32_t raw = raw_stage(is_v, it, c), st = kv_stage(is_v, it, c);
+        ok = w.wait_warp(bar_raw_full + 8 * raw, raw_phase(it, c) & 1);
+        if (ok) ok = w.wait_warp(bar_kv_empty + 8 * st, (kv_phase(it, c) & 1) ^ 1);
         if (!ok) break;
-        const uint32_t src = smem_base + kSmemRaw + raw * kRawBytes + row * 128, dst = sKV + st * kTileBytes + row * 128;
+        const uint32_t src = raw_buffer(raw) + row * 128, dst = sKV + st * kTileBytes + row * 128;
         if (__all_sync(0xFFFFFFFFu, __vcmpgtu4(word, 0x86868686u) == 0u)) decode_row<false>(src, dst, word, swizzle);
         else decode_row<true>(src, dst, word, swizzle);
         fence_proxy_async();
@@ -465,7 +482,15 @@ window_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
           mbar_arrive(bar_raw_empty + 8 * raw);
         }
       }
+      c0 += tiles;
     }
+  };
+
+  if (kQ8 && warp >= 12) {
+    // ---------------------------------------------------------------- decoders
+    reg_dealloc_decode();
+    grid_wait();
+    decode_tiles(tid - 384, false);
   } else if (warp >= 8) {
     reg_dealloc_service<kQ8>();
     if (warp == 10 && lane == 0) {
@@ -478,7 +503,7 @@ window_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       grid_wait();
       Sched sched(p, static_cast<int>(blockIdx.x));
       Seg s;
-      uint32_t kv_it = 0, q_it[2] = {0, 0};
+      uint32_t kv_it = 0, q_it[2] = {0, 0}, kv_c[2] = {0, 0};   // kv_c: kQ8, K and V tiles
       bool ok = true;
       while (ok && sched.next(s)) {
         auto load_q = [&](int a) {
@@ -494,12 +519,13 @@ window_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         };
         auto load_kv = [&](const TileInfo& ti, int kv) {
           if constexpr (kQ8) {
-            const uint32_t raw = kv_it % kRawStages, bar = bar_raw_full + 8 * raw;
-            if (ok) ok = w.wait(bar_raw_empty + 8 * raw, ((kv_it / kRawStages) & 1) ^ 1);
+            const uint32_t raw = raw_stage(kv == 1, kv_it, kv_c[kv]), bar = bar_raw_full + 8 * raw;
+            if (ok) ok = w.wait(bar_raw_empty + 8 * raw, (raw_phase(kv_it, kv_c[kv]) & 1) ^ 1);
             if (!ok) return;
             mbar_expect_tx(bar, kRawBytes);
-            tma_load_4d(smem_base + kSmemRaw + raw * kRawBytes, kv == 0 ? &tm_kf : &tm_vf, bar, 0, s.h, ti.row, s.b);
+            tma_load_4d(raw_buffer(raw), kv == 0 ? &tm_kf : &tm_vf, bar, 0, s.h, ti.row, s.b);
             ++kv_it;
+            ++kv_c[kv];
             return;
           }
           const uint32_t st = kv_it % kStages;
@@ -549,14 +575,14 @@ window_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         const int n = s.t1 - s.t0;
         const ValidKeys valid_of(p, s.b);
         for (int j = 0; j < n; ++j) {
-          const uint32_t it = kv_base + (j > 0 ? 2 * j - 1 : 0), st = it % kStages;   // K's place in the order
+          const uint32_t it = kv_base + (j > 0 ? 2 * j - 1 : 0), st = kv_stage(false, it, kv_base / 2 + j);   // K's place in the order
           const int valid = valid_of(s.t0 + j);
           const uint32_t idesc = valid == kTileN ? idesc_full : idesc_bf16_f32(kTileM, (valid + 15) & ~15, 0);
           const uint64_t dk = dk0 + static_cast<uint64_t>((st * kTileBytes) >> 4);
 #pragma unroll 1
           for (int a = 0; a < s.nq; ++a) {
             if (ok && j == 0) ok = w.wait_warp(bar_q_full + 8 * a, (a == 0 ? q0 : q1) & 1);
-            if (ok && a == 0) ok = w.wait_warp(bar_kv_full + 8 * st, (it / kStages) & 1);
+            if (ok && a == 0) ok = w.wait_warp(bar_kv_full + 8 * st, kv_phase(it, kv_base / 2 + j) & 1);
             TRACE(2, n0 + n1, 0);
             if (before >= 0) s_free_sync(before, (before == 0 ? n0 : n1) - 1);
             TRACE(2, n0 + n1, 1);
@@ -593,10 +619,10 @@ window_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         const int n = s.t1 - s.t0;
         const ValidKeys valid_of(p, s.b);
         for (int j = 0; j < n; ++j) {
-          const uint32_t it = kv_base + (j + 1 < n ? 2 * j + 2 : 2 * n - 1), st = it % kStages;
+          const uint32_t it = kv_base + (j + 1 < n ? 2 * j + 2 : 2 * n - 1), st = kv_stage(true, it, kv_base / 2 + j);
           const int k_steps = (valid_of(s.t0 + j) + 15) >> 4;
           const uint64_t dv = dv0 + static_cast<uint64_t>((st * kTileBytes) >> 4);
-          if (ok) ok = w.wait_warp(bar_kv_full + 8 * st, (it / kStages) & 1);
+          if (ok) ok = w.wait_warp(bar_kv_full + 8 * st, kv_phase(it, kv_base / 2 + j) & 1);
 #pragma unroll 1
           for (int a = 0; a < s.nq; ++a) {
             const uint32_t o_tmem = tmem_base + kTmemO + a * 128, p_tmem = tmem_base + kTmemP + a * 64;
@@ -637,6 +663,7 @@ window_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     const int row = tid & 127;             // row inside the tile = TMEM lane
     const uint32_t t_lane = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16);
     const uint32_t t_S = t_lane + kTmemS, t_P = t_lane + kTmemP + a * 64, t_O = t_lane + kTmemO + a * 128;
+    if (lone && a == 1) decode_tiles(row, true);
     Sched sched(p, static_cast<int>(blockIdx.x));
     Seg s;
     Seg seg = {};        // of a cluster's block: its only one
@@ -1071,15 +1098,14 @@ static bool make_map(CUtensorMap* m, const void* base, int rank, const uint64_t*
 struct DeviceInfo {
   bool ok = false;
   int sm_count = 0;
-  int32_t clusters[2][kMaxClusterParts + 1] = {};   // clusters of that many blocks which the device runs at the same
-                                                    // time, of the kernel over a bf16 and of that over an 8-bit cache
-  int32_t few_blocks[2] = {};   // blocks of the kernel for few queries that an SM holds
+  int32_t clusters[kKinds][kMaxClusterParts + 1] = {};   // clusters of that many blocks which the device runs at the same time
+  int32_t few_blocks = 0;   // blocks of the kernel for few queries that an SM holds
 };
 
-template <bool kQ8>
+template <Kind kKind>
 static bool query_kernels(int32_t* clusters) {
-  if (cudaFuncSetAttribute(window_attn_kernel<false, kQ8>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttnSmemBytes) != cudaSuccess ||
-      cudaFuncSetAttribute(window_attn_kernel<true, kQ8>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttnSmemBytes) != cudaSuccess)
+  if (cudaFuncSetAttribute(window_attn_kernel<false, kKind>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttnSmemBytes) != cudaSuccess ||
+      cudaFuncSetAttribute(window_attn_kernel<true, kKind>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttnSmemBytes) != cudaSuccess)
     return false;
   for (int parts = 2; parts <= kMaxClusterParts; ++parts) {
     cudaLaunchAttribute attr;
@@ -1088,12 +1114,12 @@ static bool query_kernels(int32_t* clusters) {
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(parts);
-    cfg.blockDim = dim3(Form<kQ8>::kThreads);
+    cfg.blockDim = dim3(Form<kKind != kBf16>::kThreads);
     cfg.dynamicSmemBytes = kAttnSmemBytes;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
     int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, window_attn_kernel<true, kQ8>, &cfg) == cudaSuccess) clusters[parts] = n;
+    if (cudaOccupancyMaxActiveClusters(&n, window_attn_kernel<true, kKind>, &cfg) == cudaSuccess) clusters[parts] = n;
     else cudaGetLastError();   // no clusters of that size, then
   }
   return true;
@@ -1108,7 +1134,8 @@ static DeviceInfo query_device(int dev) {
   if (it != known.end()) return it->second;
   DeviceInfo info;
   info.ok = cudaDeviceGetAttribute(&info.sm_count, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess &&
-            query_kernels<false>(info.clusters[0]) && query_kernels<true>(info.clusters[1]) && few_setup(info.few_blocks);
+            query_kernels<kBf16>(info.clusters[kBf16]) &&
+            query_kernels<kQ8Pairs>(info.clusters[kQ8Pairs]) && query_kernels<kQ8Lone>(info.clusters[kQ8Lone]) && few_setup(&info.few_blocks);
   if (!info.ok) return info;
   return known[dev] = info;
 }
@@ -1262,15 +1289,16 @@ constexpr int kOverlapSteps = 64;   // key-tile steps per worker below which a l
 // The overlap saves 1.5-6 thousand cycles of a launch at any length; at the cap the clock falls for
 // the idling it takes away.  The line lies about where the gain of short runs (0.6 % at 57 steps) has
 // come down to the loss of runs at the cap (0.4 %).
-static int launch_attn(const AttnParams& p, bool q8, const CUtensorMap& tm_q, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
+static int launch_attn(const AttnParams& p, Kind kind, const CUtensorMap& tm_q, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
                        const CUtensorMap& tm_kf, const CUtensorMap& tm_vf, __nv_bfloat16* out, cudaStream_t st) {
   const bool brief = p.all_steps < static_cast<int64_t>(kOverlapSteps) * p.n_workers;
   const cudaError_t err =
       launch_clusters(brief, p.cluster ? p.parts : 1,
-                      q8 ? (p.cluster ? window_attn_kernel<true, true> : window_attn_kernel<false, true>)
-                         : (p.cluster ? window_attn_kernel<true, false> : window_attn_kernel<false, false>),
-                      p.n_workers, q8 ? Form<true>::kThreads : Form<false>::kThreads, kAttnSmemBytes, st, tm_q, tm_k, tm_v,
-                      tm_kf, tm_vf, p, out);
+                      kind == kBf16      ? (p.cluster ? window_attn_kernel<true, kBf16> : window_attn_kernel<false, kBf16>)
+                      : kind == kQ8Pairs ? (p.cluster ? window_attn_kernel<true, kQ8Pairs> : window_attn_kernel<false, kQ8Pairs>)
+                                         : (p.cluster ? window_attn_kernel<true, kQ8Lone> : window_attn_kernel<false, kQ8Lone>),
+                      p.n_workers, kind == kBf16 ? Form<false>::kThreads : Form<true>::kThreads, kAttnSmemBytes, st, tm_q, tm_k,
+                      tm_v, tm_kf, tm_vf, p, out);
   g_launches.fetch_add(1);
   return err == cudaSuccess ? UNSTEP_OK : UNSTEP_ERR_CUDA;
 }
@@ -1320,12 +1348,13 @@ static int window_attn_run(const unstep_shape_t* shape, const int32_t* start_fra
 
   AttnParams p;
   plan_shape(p, shape, sink_frames);
+  const Kind kind = !q8 ? kBf16 : p.q_tiles == 1 ? kQ8Lone : kQ8Pairs;
   if (q8) p.flat = 1;
   p.cache_rows = static_cast<int64_t>(C * T);
   for (int b0 = 0; b0 < shape->batch; b0 += kMaxStreamsPerLaunch) {
     const int nb = shape->batch - b0 < kMaxStreamsPerLaunch ? shape->batch - b0 : kMaxStreamsPerLaunch;
     rc = plan_launch(p, shape, start_frame + b0, nb, window_frames, sink_frames, sink_attend, info.sm_count,
-                     info.clusters[q8]);
+                     info.clusters[kind]);
     if (rc != UNSTEP_OK) return rc;
     rc = bind_scratch(p, st, scratch, info.sm_count, out, 0);
     if (rc != UNSTEP_OK) return rc;
@@ -1352,7 +1381,7 @@ static int window_attn_run(const unstep_shape_t* shape, const int32_t* start_fra
     } else if (!make_map(&tm_k, kb, 5, rdims, rstr, 2) || !make_map(&tm_v, vb, 5, rdims, rstr, 2)) {
       return UNSTEP_ERR_CUDA;
     }
-    rc = launch_attn(p, q8, tm_q, tm_k, tm_v, tm_kf, tm_vf, ob, st);
+    rc = launch_attn(p, kind, tm_q, tm_k, tm_v, tm_kf, tm_vf, ob, st);
     if (rc != UNSTEP_OK) return rc;
   }
   return UNSTEP_OK;
@@ -1388,7 +1417,7 @@ extern "C" int unstep_window_attn_sink(const unstep_shape_t* shape, int32_t sink
 }
 
 // Query-tile pairs of a head from which on the window of an 8-bit cache is unpacked in front of the attention.
-constexpr int kUnpackPairs = 5;
+constexpr int kUnpackPairs = 4;
 
 // Attention over an 8-bit cache with few queries, or with many, by way of unpacked windows, as many heads at a time as the
 // scratch holds.  Leaves `done` false where the kernel that decodes tiles for itself is to do it.  With many queries every
@@ -1471,7 +1500,7 @@ static int window_attn_q8_run(const unstep_shape_t* shape, int32_t sink_frames, 
     for (int64_t h0 = 0; h0 < Hn; h0 += heads) {
       const int64_t g = Hn - h0 < heads ? Hn - h0 : heads;
       p.items_per_stream = static_cast<int32_t>(g) * p.q_pairs;
-      plan_split(p, info.sm_count, info.clusters[0]);
+      plan_split(p, info.sm_count, info.clusters[kBf16]);
       uint8_t* const window_v = window + nb * g * rows * kHeadDim * 2;
       u.head0 = static_cast<int32_t>(h0);
       u.extent = nb * g * rows * (kHeadDim / 8);
@@ -1495,7 +1524,7 @@ static int window_attn_q8_run(const unstep_shape_t* shape, int32_t sink_frames, 
       if (!make_map(&tm_q, qb, 4, qdims, qstr, 2) || !make_map(&tm_k, window, 4, wdims, wstr, 2) ||
           !make_map(&tm_v, window_v, 4, wdims, wstr, 2))
         return UNSTEP_ERR_CUDA;
-      rc = launch_attn(p, false, tm_q, tm_k, tm_v, tm_k, tm_v, reinterpret_cast<__nv_bfloat16*>(ob), st);
+      rc = launch_attn(p, kBf16, tm_q, tm_k, tm_v, tm_k, tm_v, reinterpret_cast<__nv_bfloat16*>(ob), st);
       if (rc != UNSTEP_OK) return rc;
     }
   }
@@ -1603,7 +1632,7 @@ extern "C" int unstep_attn_clusters(int32_t* clusters) {
   if (rc != UNSTEP_OK) return rc;
   const DeviceInfo& info = device_info();
   if (!info.ok) return UNSTEP_ERR_CUDA;
-  for (int n = 0; n <= kMaxClusterParts; ++n) clusters[n] = info.clusters[0][n];
+  for (int n = 0; n <= kMaxClusterParts; ++n) clusters[n] = info.clusters[kBf16][n];
   return UNSTEP_OK;
 }
 

@@ -1,4 +1,4 @@
-// Attention of at most 16 queries a stream over an 8-bit cache (sm_100a): single tokens, and what little more goes with them.
+// Attention of at most 8 queries a stream over an 8-bit cache (sm_100a): single tokens, and what little more goes with them.
 //
 // DRAM bound: every cached key and value is read once, and a query tile of the tensor-memory kernel would be next to empty,
 // while it waits for tiles to be decoded into shared memory.  Here a warp takes 16 keys at a time straight from global memory
@@ -59,23 +59,16 @@ __device__ __forceinline__ uint2 spread_pairs(uint32_t w) {
 __device__ __forceinline__ uint32_t factor_small(uint32_t byte) { return byte * 0x00800080u + 120u * 0x00800080u; }
 
 // What a warp leaves in shared memory: O as [query][dim], then (m, l).
-template <int kN>   // groups of 8 queries
-__host__ __device__ constexpr int few_warp_bytes() {
-  return 8 * kN * (kHeadDim + 2) * static_cast<int>(sizeof(float));
-}
+constexpr int kFewWarpBytes = kFewQueries * (kHeadDim + 2) * static_cast<int>(sizeof(float));
 // A block's part in the scratch: O as [query][dim], then (m, l) as [query].
-template <int kN>
-__host__ __device__ constexpr int few_part_floats() {
-  return 8 * kN * kHeadDim + 8 * kN * 2;
-}
+constexpr int kFewPartFloats = kFewQueries * kHeadDim + kFewQueries * 2;
 
-template <int kN>
-__global__ void __launch_bounds__(kFewThreads, kN == 1 ? 2 : 1)
+__global__ void __launch_bounds__(kFewThreads, 2)
 window_attn_few_kernel(const __grid_constant__ FewParams p, const uint4* q_rot, const uint4* cache_k, const uint8_t* scale_k,
                        const uint4* cache_v, const uint8_t* scale_v, uint32_t* out) {
-  extern __shared__ __align__(16) uint8_t few_smem[];
-  auto slab = [&](int w, int query) { return reinterpret_cast<float*>(few_smem + w * few_warp_bytes<kN>()) + query * kHeadDim; };
-  auto slab_ml = [&](int w) { return reinterpret_cast<float2*>(slab(w, 8 * kN)); };
+  __shared__ __align__(16) uint8_t few_smem[kFewWarps * kFewWarpBytes];
+  auto slab = [&](int w, int query) { return reinterpret_cast<float*>(few_smem + w * kFewWarpBytes) + query * kHeadDim; };
+  auto slab_ml = [&](int w) { return reinterpret_cast<float2*>(slab(w, kFewQueries)); };
   __shared__ int last;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
@@ -102,29 +95,19 @@ window_attn_few_kernel(const __grid_constant__ FewParams p, const uint4* q_rot, 
   const uint4* const head_q = q_rot + (b * (static_cast<int64_t>(p.L) - p.cache_rows) * p.Hn + head) * 16;
   const uint32_t row_codes = 8u * p.Hn, row_scales = 4u * p.Hn;
 
-  // B of S^T: thread (g, c) has query g, dims 32 c ..
-  uint32_t q[kN][16];
+  // B of S^T: thread (g, c) has query g, dims 32 c .. in pairs (0, 2) and (1, 3) of four, as spread_pairs makes them
+  uint32_t q[16];
 #pragma unroll
-  for (int n = 0; n < kN; ++n) {
-    const int query = 8 * n + g;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      uint4 x = make_uint4(0, 0, 0, 0);
-      if (query < p.L) x = __ldca(head_q + static_cast<int64_t>(query) * p.Hn * 16 + 4 * c + i);
-      // pairs (0, 2) and (1, 3) of four dims, as spread_pairs makes them
-      q[n][4 * i] = __byte_perm(x.x, x.y, 0x5410), q[n][4 * i + 1] = __byte_perm(x.x, x.y, 0x7632);
-      q[n][4 * i + 2] = __byte_perm(x.z, x.w, 0x5410), q[n][4 * i + 3] = __byte_perm(x.z, x.w, 0x7632);
-    }
+  for (int i = 0; i < 4; ++i) {
+    uint4 x = make_uint4(0, 0, 0, 0);
+    if (g < p.L) x = __ldca(head_q + static_cast<int64_t>(g) * p.Hn * 16 + 4 * c + i);
+    q[4 * i] = __byte_perm(x.x, x.y, 0x5410), q[4 * i + 1] = __byte_perm(x.x, x.y, 0x7632);
+    q[4 * i + 2] = __byte_perm(x.z, x.w, 0x5410), q[4 * i + 3] = __byte_perm(x.z, x.w, 0x7632);
   }
-  float o[kN][8][4];   // O^T: dims 16 g + 2 t and + 2 t + 1, queries 8 n + 2 c and + 1
-  float m[kN][2], l[kN][2];
+  float o[8][4];   // O^T: dims 16 g + 2 t and + 2 t + 1, queries 2 c and + 1
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 #pragma unroll
-  for (int n = 0; n < kN; ++n) {
-    m[n][0] = m[n][1] = -INFINITY;
-    l[n][0] = l[n][1] = 0.f;
-#pragma unroll
-    for (int t = 0; t < 8; ++t) o[n][t][0] = o[n][t][1] = o[n][t][2] = o[n][t][3] = 0.f;
-  }
+  for (int t = 0; t < 8; ++t) o[t][0] = o[t][1] = o[t][2] = o[t][3] = 0.f;
 
   // codes of keys g, g + 8 (dims 32 c ..) and of keys 2 c, 2 c + 1, 2 c + 8, 2 c + 9 (dims 16 g ..), a step ahead
   uint32_t xk[2][8];
@@ -191,9 +174,7 @@ window_attn_few_kernel(const __grid_constant__ FewParams p, const uint4* q_rot, 
   }
 #pragma unroll 1
   for (; step < hi; step += kFewWarps) {
-    float s[kN][4];
-#pragma unroll
-    for (int n = 0; n < kN; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
     // one factor up to a scale byte of 134, else 2^120 and another
     const bool two_k = __any_sync(0xFFFFFFFFu, max(ek[0], ek[1]) > 134u);
     {
@@ -212,61 +193,49 @@ window_attn_few_kernel(const __grid_constant__ FewParams p, const uint4* q_rot, 
             y[i].y = q8::mul_bf16x2(y[i].y, q8::factor2(ek[i]));
           }
         }
-#pragma unroll
-        for (int n = 0; n < kN; ++n) mma16816(s[n], y[0].x, y[1].x, y[0].y, y[1].y, q[n][2 * w], q[n][2 * w + 1]);
+        mma16816(s, y[0].x, y[1].x, y[0].y, y[1].y, q[2 * w], q[2 * w + 1]);
       }
     }
     const int next = step + kFewWarps;
     if (next < hi) load_k(next);
     const int left = keys - step * kFewKeys;   // keys of this step
+    if (g >= left) s[0] = s[1] = -INFINITY;
+    if (g + 8 >= left) s[2] = s[3] = -INFINITY;
     bool jump = first;
 #pragma unroll
-    for (int n = 0; n < kN; ++n) {
-      if (g >= left) s[n][0] = s[n][1] = -INFINITY;
-      if (g + 8 >= left) s[n][2] = s[n][3] = -INFINITY;
-#pragma unroll
-      for (int e = 0; e < 2; ++e) jump = jump || (fmaxf(s[n][e], s[n][2 + e]) - m[n][e]) * p.scale_log2e > kFewJump;
-    }
+    for (int e = 0; e < 2; ++e) jump = jump || (fmaxf(s[e], s[2 + e]) - m[e]) * p.scale_log2e > kFewJump;
     // The reference is the first step's maximum, and moves only where a score is far above it: up to there weights and
     // sums have the precision that they have near 1.
     if (__builtin_expect(__any_sync(0xFFFFFFFFu, jump), 0)) {
       first = false;
-#pragma unroll
-      for (int n = 0; n < kN; ++n) {
-        float alpha[2];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          float top = fmaxf(s[n][e], s[n][2 + e]);
-#pragma unroll
-          for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-          const float now = fmaxf(m[n][e], top);
-          alpha[e] = ex2((m[n][e] - now) * p.scale_log2e);
-          m[n][e] = now;
-          l[n][e] *= alpha[e];
-        }
-#pragma unroll
-        for (int t = 0; t < 8; ++t) {
-          o[n][t][0] *= alpha[0];
-          o[n][t][1] *= alpha[1];
-          o[n][t][2] *= alpha[0];
-          o[n][t][3] *= alpha[1];
-        }
-      }
-    }
-    uint32_t pt[kN][2];
-#pragma unroll
-    for (int n = 0; n < kN; ++n) {
+      float alpha[2];
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const float ref = m[n][e] * p.scale_log2e;
-        s[n][e] = ex2(fmaf(s[n][e], p.scale_log2e, -ref));
-        s[n][2 + e] = ex2(fmaf(s[n][2 + e], p.scale_log2e, -ref));
-        l[n][e] += s[n][e] + s[n][2 + e];
+        float top = fmaxf(s[e], s[2 + e]);
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+        const float now = fmaxf(m[e], top);
+        alpha[e] = ex2((m[e] - now) * p.scale_log2e);
+        m[e] = now;
+        l[e] *= alpha[e];
       }
-      // P is rounded to bf16, as the operand that the matrix product takes
-      pt[n][0] = transpose8x8(pack_bf16x2(s[n][0], s[n][1]));
-      pt[n][1] = transpose8x8(pack_bf16x2(s[n][2], s[n][3]));
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        o[t][0] *= alpha[0];
+        o[t][1] *= alpha[1];
+        o[t][2] *= alpha[0];
+        o[t][3] *= alpha[1];
+      }
     }
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const float ref = m[e] * p.scale_log2e;
+      s[e] = ex2(fmaf(s[e], p.scale_log2e, -ref));
+      s[2 + e] = ex2(fmaf(s[2 + e], p.scale_log2e, -ref));
+      l[e] += s[e] + s[2 + e];
+    }
+    // P is rounded to bf16, as the operand that the matrix product takes
+    const uint32_t pt0 = transpose8x8(pack_bf16x2(s[0], s[1])), pt1 = transpose8x8(pack_bf16x2(s[2], s[3]));
     const bool two_v = __any_sync(0xFFFFFFFFu, max(max(ev[0], ev[1]), max(ev[2], ev[3])) > 134u);
     {
       // factors of the two keys of a pair side by side
@@ -290,8 +259,7 @@ window_attn_few_kernel(const __grid_constant__ FewParams p, const uint4* q_rot, 
             y[i].y = q8::mul_bf16x2(y[i].y, f2);
           }
         }
-#pragma unroll
-        for (int n = 0; n < kN; ++n) mma16816(o[n][w], y[0].x, y[0].y, y[1].x, y[1].y, pt[n][0], pt[n][1]);
+        mma16816(o[w], y[0].x, y[0].y, y[1].x, y[1].y, pt0, pt1);
       }
     }
     if (next < hi) load_v(next);
@@ -299,18 +267,15 @@ window_attn_few_kernel(const __grid_constant__ FewParams p, const uint4* q_rot, 
 
   // ---- warps of the block ----
 #pragma unroll
-  for (int n = 0; n < kN; ++n) {
+  for (int e = 0; e < 2; ++e) {
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
+    for (int d = 4; d < 32; d <<= 1) l[e] += __shfl_xor_sync(0xFFFFFFFFu, l[e], d);
+    const int query = 2 * c + e;
+    if (g == 0) slab_ml(warp)[query] = make_float2(m[e], l[e]);
+    if (query < p.L) {
+      float* const to = slab(warp, query) + 16 * g;
 #pragma unroll
-      for (int d = 4; d < 32; d <<= 1) l[n][e] += __shfl_xor_sync(0xFFFFFFFFu, l[n][e], d);
-      const int query = 8 * n + 2 * c + e;
-      if (g == 0) slab_ml(warp)[query] = make_float2(m[n][e], l[n][e]);
-      if (query < p.L) {
-        float* const to = slab(warp, query) + 16 * g;
-#pragma unroll
-        for (int t = 0; t < 8; ++t) *reinterpret_cast<float2*>(to + 2 * t) = make_float2(o[n][t][e], o[n][t][2 + e]);
-      }
+      for (int t = 0; t < 8; ++t) *reinterpret_cast<float2*>(to + 2 * t) = make_float2(o[t][e], o[t][2 + e]);
     }
   }
   __syncthreads();
@@ -330,25 +295,26 @@ window_attn_few_kernel(const __grid_constant__ FewParams p, const uint4* q_rot, 
   constexpr int kCols = kHeadDim / 4;
   float4* const part4 = reinterpret_cast<float4*>(p.part);
   float2* const part2 = reinterpret_cast<float2*>(p.part);
-  constexpr int kPart4 = few_part_floats<kN>() / 4, kMl2 = 8 * kN * kHeadDim / 2, kPart2 = few_part_floats<kN>() / 2;
-  // the warps' results in shared memory as one, to the scratch or to the result
-  auto merge_warps = [&](bool to_scratch) {
+  constexpr int kPart4 = kFewPartFloats / 4, kMl2 = kFewQueries * kHeadDim / 2, kPart2 = kFewPartFloats / 2;
+  // the first `slabs` results in shared memory as one, to the scratch or to the result
+  auto merge_slabs = [&](int slabs, bool to_scratch) {
     for (int i = threadIdx.x; i < p.L * kCols; i += kFewThreads) {
       const int query = i / kCols, col = i - query * kCols;
       float all = -INFINITY, sum = 0.f;
       float2 ml[kFewWarps];
 #pragma unroll
       for (int w = 0; w < kFewWarps; ++w) {
-        ml[w] = slab_ml(w)[query];
+        ml[w] = w < slabs ? slab_ml(w)[query] : make_float2(-INFINITY, 0.f);
         all = fmaxf(all, ml[w].x);
       }
       float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int w = 0; w < kFewWarps; ++w) {
-        const float f = weight(ml[w].x, all);
-        sum = fmaf(ml[w].y, f, sum);
-        add(acc, reinterpret_cast<const float4*>(slab(w, query))[col], f);
-      }
+      for (int w = 0; w < kFewWarps; ++w)
+        if (w < slabs) {
+          const float f = weight(ml[w].x, all);
+          sum = fmaf(ml[w].y, f, sum);
+          add(acc, reinterpret_cast<const float4*>(slab(w, query))[col], f);
+        }
       if (to_scratch) {
         UNSTEP_STORE(part4, static_cast<int64_t>(block) * kPart4 + i, p.extent_part / 4, acc, p.status);
         if (col == 0)
@@ -358,7 +324,7 @@ window_attn_few_kernel(const __grid_constant__ FewParams p, const uint4* q_rot, 
       }
     }
   };
-  merge_warps(parts > 1);
+  merge_slabs(kFewWarps, parts > 1);
   if (parts == 1) return;
   // ---- blocks of the item ----
   const int64_t counter = static_cast<int64_t>(b) * p.Hn + h;
@@ -378,41 +344,38 @@ window_attn_few_kernel(const __grid_constant__ FewParams p, const uint4* q_rot, 
   __syncthreads();
   if (!last) return;
   __threadfence();   // acquire side for every thread that reads the other parts below
-  // every warp merges its share of the parts, a lane four dims, and then the warps merge as above
+  // A warp has a query (the warps that are left over share the parts of one), a lane four dims of it, and what the
+  // warps of a query have is merged as above.
   const int64_t part0 = block - part;
-  for (int query = 0; query < p.L; ++query) {
+  const int shares = p.L <= 1 ? 8 : p.L <= 2 ? 4 : p.L <= 4 ? 2 : 1, query = warp / shares, share = warp - query * shares;
+  if (query < p.L) {
     float all = -INFINITY, sum = 0.f;
 #pragma unroll 4
-    for (int k = warp; k < parts; k += kFewWarps) all = fmaxf(all, __ldcg(part2 + (part0 + k) * kPart2 + kMl2 + query).x);
+    for (int k = share; k < parts; k += shares) all = fmaxf(all, __ldcg(part2 + (part0 + k) * kPart2 + kMl2 + query).x);
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-    for (int k = warp; k < parts; k += kFewWarps) {
+    for (int k = share; k < parts; k += shares) {
       const float2 ml = __ldcg(part2 + (part0 + k) * kPart2 + kMl2 + query);
       const float f = weight(ml.x, all);
       sum = fmaf(ml.y, f, sum);
       add(acc, __ldcg(part4 + (part0 + k) * kPart4 + query * kCols + lane), f);
     }
-    reinterpret_cast<float4*>(slab(warp, query))[lane] = acc;
-    if (lane == 0) slab_ml(warp)[query] = make_float2(all, sum);
+    reinterpret_cast<float4*>(slab(share, query))[lane] = acc;
+    if (lane == 0) slab_ml(share)[query] = make_float2(all, sum);
   }
   __syncthreads();
-  merge_warps(false);
+  merge_slabs(shares, false);
 }
 
-template <int kN>
-static bool few_query(int32_t* blocks) {
+bool few_setup(int32_t* blocks_per_sm) {
   int n = 0;
-  if (cudaFuncSetAttribute(window_attn_few_kernel<kN>, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewWarps * few_warp_bytes<kN>()) != cudaSuccess ||
-      cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, window_attn_few_kernel<kN>, kFewThreads, kFewWarps * few_warp_bytes<kN>()) != cudaSuccess)
-    return false;
-  *blocks = n;
+  if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, window_attn_few_kernel, kFewThreads, 0) != cudaSuccess) return false;
+  *blocks_per_sm = n;
   return n > 0;
 }
-bool few_setup(int32_t* blocks_per_sm) { return few_query<1>(blocks_per_sm) && few_query<2>(blocks_per_sm + 1); }
 
-int launch_few(const AttnParams& a, int nb, int sm_count, const int32_t* blocks_per_sm, const void* q_rot, const void* cache_k,
+int launch_few(const AttnParams& a, int nb, int sm_count, int32_t blocks_per_sm, const void* q_rot, const void* cache_k,
                const void* scale_k, const void* cache_v, const void* scale_v, void* out, cudaStream_t st) {
-  const bool one = a.L <= 8;
   FewParams p;
   p.Hn = a.Hn;
   p.L = a.L;
@@ -438,8 +401,8 @@ int launch_few(const AttnParams& a, int nb, int sm_count, const int32_t* blocks_
   }
   // The shortest share of steps for a block with which all blocks run at once (a second wave would take as long as
   // the first), but at least one for each of its warps; with more items than blocks an item is not split.
-  const int64_t room = static_cast<int64_t>(sm_count) * blocks_per_sm[one ? 0 : 1];
-  const int64_t part_room = p.extent_part / (one ? few_part_floats<1>() : few_part_floats<2>());
+  const int64_t room = static_cast<int64_t>(sm_count) * blocks_per_sm;
+  const int64_t part_room = p.extent_part / kFewPartFloats;
   int64_t share = (all + room - 1) / room, blocks = 0;
   if (share < kFewWarps) share = kFewWarps;
   for (int i = 0; i < nb; ++i)   // and no more than kFewParts blocks, which one of them merges
@@ -457,8 +420,7 @@ int launch_few(const AttnParams& a, int nb, int sm_count, const int32_t* blocks_
     if (!split || (blocks <= room && blocks <= part_room)) break;
   }
   const cudaError_t err = launch_overlapped(
-      true, one ? window_attn_few_kernel<1> : window_attn_few_kernel<2>, dim3(static_cast<unsigned>(blocks)), kFewThreads,
-      one ? kFewWarps * few_warp_bytes<1>() : kFewWarps * few_warp_bytes<2>(), st, p, static_cast<const uint4*>(q_rot),
+      true, window_attn_few_kernel, dim3(static_cast<unsigned>(blocks)), kFewThreads, 0, st, p, static_cast<const uint4*>(q_rot),
       static_cast<const uint4*>(cache_k), static_cast<const uint8_t*>(scale_k), static_cast<const uint4*>(cache_v),
       static_cast<const uint8_t*>(scale_v), static_cast<uint32_t*>(out));
   g_launches.fetch_add(1);

@@ -417,12 +417,11 @@ inline void plan_shape(AttnParams& p, const unstep_shape_t* shape, int32_t sink_
   p.cache_rows = 0;
 }
 
-// The kernel for launches of at most kFewQueries queries a stream over an 8-bit cache (attn_few.cu): its attributes on the
-// current device and how many of its blocks an SM holds (up to 8 queries, up to 16), and a launch over the windows and
-// with the scratch of `a`.  Host only.
-constexpr int kFewQueries = 16;
+// The kernel for launches of at most kFewQueries queries a stream over an 8-bit cache (attn_few.cu): how many of its blocks
+// an SM of the current device holds, and a launch over the windows and with the scratch of `a`.  Host only.
+constexpr int kFewQueries = 8;
 bool few_setup(int32_t* blocks_per_sm);
-int launch_few(const AttnParams& a, int nb, int sm_count, const int32_t* blocks_per_sm, const void* q_rot, const void* cache_k,
+int launch_few(const AttnParams& a, int nb, int sm_count, int32_t blocks_per_sm, const void* q_rot, const void* cache_k,
                const void* scale_k, const void* cache_v, const void* scale_v, void* out, cudaStream_t st);
 
 // Argument checks shared by the attention entry points and the plan entry point (no device needed).

@@ -245,7 +245,7 @@ def test_attention(name):
         q = q.flip(1).contiguous()
 
 
-# Up to 16 queries a stream: keys go straight from memory into warp-level products.
+# Up to 8 queries a stream: keys go straight from memory into warp-level products.
 FEW = [
     ("8_queries_one_key", (1, 1, (1, 8), 1, 1, 0, 1, 0, (0,))),
     ("9_queries", (2, 3, (3, 3), 1, 40, 2, 33, 1, (100, 7))),
@@ -318,8 +318,8 @@ def test_attention_over_unpacked_windows(name):
 
 
 def test_heads_in_groups_where_the_unpacked_windows_exceed_the_scratch():
-    # 40 heads x 13 200 keys x 512 bytes are 270 MB: two groups of 20 heads; and streams one by one
-    for batch, heads, frames in ((1, 40, 12), (2, 17, 12)):
+    # 40 heads x 13 200 keys x 512 bytes are 270 MB: two groups of 20 heads; three streams of 17 heads: 9 and 8 heads of each
+    for batch, heads, frames in ((1, 40, 12), (3, 17, 12)):
         sh = shape(batch, heads, 1, 11, 100, frames)
         layer = Layer(sh)
         layer.fill_codes(53)
