@@ -486,11 +486,13 @@ window_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     }
   };
 
-  if (kQ8 && warp >= 12) {
+  const bool softmax_role = lone ? warp < 4 : warp < 8;
+  if (kQ8 && (warp >= 12 || (lone && !softmax_role && warp < 8))) {
     // ---------------------------------------------------------------- decoders
+    // (one copy of the code for both groups of a lone launch)
     reg_dealloc_decode();
     grid_wait();
-    decode_tiles(tid - 384, false);
+    decode_tiles(tid & 127, warp < 8);
   } else if (warp >= 8) {
     reg_dealloc_service<kQ8>();
     if (warp == 10 && lane == 0) {
@@ -663,7 +665,6 @@ window_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     const int row = tid & 127;             // row inside the tile = TMEM lane
     const uint32_t t_lane = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16);
     const uint32_t t_S = t_lane + kTmemS, t_P = t_lane + kTmemP + a * 64, t_O = t_lane + kTmemO + a * 128;
-    if (lone && a == 1) decode_tiles(row, true);
     Sched sched(p, static_cast<int>(blockIdx.x));
     Seg s;
     Seg seg = {};        // of a cluster's block: its only one
@@ -904,7 +905,8 @@ window_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       cluster_sync();   // all parts are in place
       const int parts = p.parts, part = static_cast<int>(cluster_rank());
       // a lone query tile is shared out to both groups
-      const int tile = seg.nq == 2 ? a : 0, share = seg.nq == 2 ? part : 2 * part + a, shares = seg.nq == 2 ? parts : 2 * parts;
+      const bool whole_share = lone || seg.nq == 2;
+      const int tile = seg.nq == 2 ? a : 0, share = whole_share ? part : 2 * part + a, shares = whole_share ? parts : 2 * parts;
       const int n = (2 * seg.qp + tile) * kTileM + row;
       bool good = seg.nq > 0;
       for (int c = 0; c < parts; ++c)   // a block that gave up has left no part
@@ -956,7 +958,7 @@ window_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   }
   // The other roles meet the softmax groups at the cluster's barrier, and no block leaves while another reads its part.
   if (kCluster) {
-    if (warp >= 8) {
+    if (!softmax_role) {
       __syncwarp();
       cluster_sync();
     }

@@ -28,7 +28,6 @@ constexpr float kFewJump = 57.f;                // as far (log2) a score may be 
 
 struct FewParams {
   int32_t Hn, L, n_streams;
-  int32_t wide;                                 // 1: cache_k is 32-byte aligned
   int64_t cache_rows;                           // rows of a stream's cache
   float scale_log2e;
   float* part;                                  // scratch: part_floats for every block
@@ -63,6 +62,8 @@ constexpr int kFewWarpBytes = kFewQueries * (kHeadDim + 2) * static_cast<int>(si
 // A block's part in the scratch: O as [query][dim], then (m, l) as [query].
 constexpr int kFewPartFloats = kFewQueries * kHeadDim + kFewQueries * 2;
 
+// kWide: cache_k is 32-byte aligned.
+template <bool kWide>
 __global__ void __launch_bounds__(kFewThreads, 2)
 window_attn_few_kernel(const __grid_constant__ FewParams p, const uint4* q_rot, const uint4* cache_k, const uint8_t* scale_k,
                        const uint4* cache_v, const uint8_t* scale_v, uint32_t* out) {
@@ -86,8 +87,9 @@ window_attn_few_kernel(const __grid_constant__ FewParams p, const uint4* q_rot, 
     j = min(j, keys - 1);
     return static_cast<uint32_t>(j + (j < end0 ? row0 : (j < end1 ? row1 : row2)));
   };
-  // from here on everything is read, at addresses that take the wait's 0 in
-  const int64_t head = b * p.cache_rows * p.Hn + h + grid_wait();
+  // from here on everything is read, at addresses that take the wait's 0 in (through a shuffle, so that they are
+  // known to be the same in all lanes)
+  const int64_t head = b * p.cache_rows * p.Hn + h + __shfl_sync(0xFFFFFFFFu, grid_wait(), 0);
   const uint4* const head_k = cache_k + head * 8;
   const uint4* const head_v = cache_v + head * 8;
   const uint8_t* const head_ek = scale_k + head * 4;
@@ -121,7 +123,7 @@ window_attn_few_kernel(const __grid_constant__ FewParams p, const uint4* q_rot, 
     return j >= end1 ? e <= keys : (j >= end0 ? e <= end1 : e <= end0);
   };
   auto load_row = [&](const void* from, uint32_t* x) {   // 32 codes
-    if (p.wide) {
+    if (kWide) {
       ld_global_32(from, x);
     } else {
       const uint4 a = __ldcs(static_cast<const uint4*>(from)), d = __ldcs(static_cast<const uint4*>(from) + 1);
@@ -369,7 +371,7 @@ window_attn_few_kernel(const __grid_constant__ FewParams p, const uint4* q_rot, 
 
 bool few_setup(int32_t* blocks_per_sm) {
   int n = 0;
-  if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, window_attn_few_kernel, kFewThreads, 0) != cudaSuccess) return false;
+  if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, window_attn_few_kernel<true>, kFewThreads, 0) != cudaSuccess) return false;
   *blocks_per_sm = n;
   return n > 0;
 }
@@ -380,7 +382,6 @@ int launch_few(const AttnParams& a, int nb, int sm_count, int32_t blocks_per_sm,
   p.Hn = a.Hn;
   p.L = a.L;
   p.n_streams = nb;
-  p.wide = (reinterpret_cast<uintptr_t>(cache_k) & 31u) == 0;   // heads are 128 bytes
   p.cache_rows = a.cache_rows;
   p.scale_log2e = a.scale_log2e;
   p.part = a.part;
@@ -419,8 +420,9 @@ int launch_few(const AttnParams& a, int nb, int sm_count, int32_t blocks_per_sm,
     }
     if (!split || (blocks <= room && blocks <= part_room)) break;
   }
+  const bool wide = (reinterpret_cast<uintptr_t>(cache_k) & 31u) == 0;   // heads are 128 bytes
   const cudaError_t err = launch_overlapped(
-      true, window_attn_few_kernel, dim3(static_cast<unsigned>(blocks)), kFewThreads, 0, st, p, static_cast<const uint4*>(q_rot),
+      true, wide ? window_attn_few_kernel<true> : window_attn_few_kernel<false>, dim3(static_cast<unsigned>(blocks)), kFewThreads, 0, st, p, static_cast<const uint4*>(q_rot),
       static_cast<const uint4*>(cache_k), static_cast<const uint8_t*>(scale_k), static_cast<const uint4*>(cache_v),
       static_cast<const uint8_t*>(scale_v), static_cast<uint32_t*>(out));
   g_launches.fetch_add(1);

@@ -174,7 +174,7 @@ def test_inputs_of_overlapped_kernels_are_read_behind_the_wait():
         for load in re.finditer(r"__ldca\(|__ldcs\(|q_in\[|= load_coefficients", body):
             assert load.start() > wait, name
         # addresses take the wait's zero in
-        assert re.search(r"\+ behind|\+= behind|\+ grid_wait\(\)", body), name
+        assert re.search(r"\+ behind|\+= behind|\+ __shfl_sync\(0xFFFFFFFFu, grid_wait\(\), 0\)", body), name
 
 
 def test_runs_of_the_cache_are_those_of_a_walk_over_the_frames():
