@@ -16,7 +16,8 @@
  *   - Every tensor pointer is a DEVICE pointer unless the comment says HOST.
  *   - bf16 tensors are dense, row-major, 16-byte aligned; the caller owns all of
  *     them.  The only device memory the library creates is the scratch of
- *     unstep_window_attn (one buffer per stream, made on first use and kept).
+ *     unstep_window_attn (one buffer per stream, made on first use and kept) and of
+ *     unstep_window_attn_q8 (the same, and one for unpacked windows).
  *   - All work is enqueued on `cuda_stream` (a cudaStream_t passed as void*; NULL
  *     is the legacy default stream).  No call synchronises or reads device data.
  *   - Return value: 0 on success, a negative unstep_status otherwise.  Arguments
@@ -297,8 +298,13 @@ int unstep_kv_read_q8(const unstep_shape_t* shape, int32_t sink_frames, const in
 
 /*
  * unstep_window_attn_sink over such a cache: the same frames, the same softmax, the keys and values as they are read back.
- * The scratch is that of unstep_window_attn, shared with it; all it says about streams, captures and graphs holds here.
  *   q_rot, out : bf16 [B, L, Hn, 128].
+ * Scratch: that of unstep_window_attn, shared with it; all it says about streams, captures and graphs holds here.  A call with
+ * more than 768 queries a stream also unpacks the windows, as many heads at a time as fit, into a buffer of 16 to
+ * 256 MB per stream, made by the first call that needs that size and kept until unstep_shutdown (smaller ones of former
+ * calls are kept too, for graphs).  Where it cannot be made - no memory left, or inside a capture - the call decodes
+ * as it goes, which takes up to a third longer; a result may then differ in its last bits.  Calls of up to 8
+ * queries a stream read the cache without tiles.
  */
 int unstep_window_attn_q8(const unstep_shape_t* shape, int32_t sink_frames, const int32_t* start_frame,
                           int32_t recent_frames, int32_t sink_attend, const void* q_rot, const void* cache_k,

@@ -450,6 +450,7 @@ extern "C" int unstep_rotary_table(const unstep_shape_t* shape, const unstep_rop
   int rc = check_shape(shape, false, true);
   if (rc == UNSTEP_OK) rc = check_rope(rope);
   if (rc != UNSTEP_OK) return rc;
+  if (start_frame > INT32_MAX - shape->chunk_frames) return UNSTEP_ERR_INVALID_ARG;
   return table_run(shape, rope, start_frame, cos_out, sin_out, cuda_stream);
 }
 

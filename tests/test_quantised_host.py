@@ -94,7 +94,7 @@ def each_bad_pointer(call, n, scales=()):
 
 def test_pointers():
     sh, rope = good_shape(), U.Rope.make()
-    for kw in (dict(cos=None), dict(sin=FAKE + 4), dict(start=-1)):
+    for kw in (dict(cos=None), dict(sin=FAKE + 4), dict(start=-1), dict(start=2 ** 31 - 1)):
         assert table(sh, rope, **kw) == INVALID
     each_bad_pointer(lambda p: apply(sh, rope, ptrs=p), 4)
     each_bad_pointer(lambda p: append(sh, rope, ptrs=p), 10, (7, 9))
