@@ -6,6 +6,7 @@
 //   warp  8     issues S = Q K^T of both query tiles; owns TMEM
 //   warp  9     issues O += P V of both query tiles
 //   warp  10    TMA producer (one lane)
+//   warps 12-15 (8-bit cache) decode the tiles that TMA brings as codes
 // A work item is (stream, head, pair of 128-query tiles): both tiles share every K/V
 // tile.  S, P (bf16) and O live in TMEM: one S for both query tiles in turn, a P and an O for each.
 // A softmax group takes its scores into registers at once and gives S back, so that the tensor core
@@ -80,10 +81,14 @@ constexpr int kHalfBytes = 128 * 64 * 2;    // one TMA box: 128 rows x 64 bf16 (
 constexpr int kTileBytes = 2 * kHalfBytes;  // 128 x 128 bf16
 // What the kernel over a bf16 cache and the one over an 8-bit cache have of their own.  The latter has four more
 // warps, which decode the tiles that TMA brings as codes (kRawStages buffers) into the bf16 buffers that the other has TMA fill.
+// Decoding is exact (quant.cuh), so softmax and products are the same.  It takes ~420 instructions a row and tile, next to a softmax
+// that is as long as the period: 4680 queries x 32760 keys x 12 heads 951 us, without the arithmetic of decoding 785, without
+// decoding 742, the bf16 kernel 694 (runs of 20).  So launches of many queries unpack their windows in front (kUnpackPairs), and
+// this is for the others, in which a head's tiles are decoded only a few times.
 //
 // Where every item has one query tile (kQ8Lone), the second softmax group has nothing to do and the second Q buffer is free: the
 // group then decodes the V tiles and the four warps the K tiles, and K and V have a ring each, of two tiles as codes and
-// two as bf16.  (Rings that both kinds go through in turn do not do for that: a warp has to see every phase of a barrier
+// two as bf16: 100 queries x 16000 keys x 8 heads 39.9 -> 32.9 us, x 24 heads 57.4 -> 49.0.  (Rings that both kinds go through in turn do not do for that: a warp has to see every phase of a barrier
 // that it waits at, as it cannot tell one from the phase before the last.)
 constexpr int kRawStages = 2, kRawBytes = 128 * 128;
 enum Kind { kBf16, kQ8Pairs, kQ8Lone };
@@ -999,7 +1004,8 @@ __global__ void wait_limit_probe_kernel(long long limit_cycles) {
 // --------------------------------------------------------------------------
 // Keys and values of an 8-bit cache's windows as bf16, for launches that read them often: per stream and head the
 // keys of the window in order, padded with zeros to whole tiles.  A thread decodes 16 dims of k and v of kUnpackRows
-// rows, 32 apart; eight threads have a row of a head, 128 bytes in and 256 out.  DRAM bound.
+// rows, 32 apart; eight threads have a row of a head, 128 bytes in and 256 out.  DRAM bound: 32760 keys x 12 heads
+// (305 MB) 46 us, 6.6 TB/s.
 // --------------------------------------------------------------------------
 constexpr int kUnpackRows = 2;
 struct Unpack8Params {
@@ -1418,7 +1424,11 @@ extern "C" int unstep_window_attn_sink(const unstep_shape_t* shape, int32_t sink
                          get_workspace, sink_frames, sink_attend);
 }
 
-// Query-tile pairs of a head from which on the window of an 8-bit cache is unpacked in front of the attention.
+// Query-tile pairs of a head from which on the window of an 8-bit cache is unpacked in front of the attention.  Unpacking moves
+// 5 bytes a dim through DRAM whatever the queries; decoding tiles takes each query pair of a head 0.5 to 1 us a key tile.  us,
+// decoded in the kernel / unpacked: 2 pairs, 24 heads x 4000 keys 40.2 / 42.7, x 16000 108 / 125; 4 pairs, x 800 22.4 / 20.2, x
+// 4000 71.4 / 66.1, x 16000 208 / 197; 5 pairs, x 3600 81.9 / 61.7; 19 pairs, 12 heads x 32760 951 / 741.  Of few items (2 heads) the
+// two are within 5 % of each other.
 constexpr int kUnpackPairs = 4;
 
 // Attention over an 8-bit cache with few queries, or with many, by way of unpacked windows, as many heads at a time as the

@@ -10,6 +10,13 @@
 // shared memory, the blocks of an item (stream, head) through the scratch: the one that is done last reads the
 // others' parts, in part order, so the result does not depend on which one that is.  Streams of different length get
 // different numbers of blocks, which clusters could not have.
+//
+// Measured: one token each of three streams, 12 heads, 4096, 1235 and 4096 keys (30 MB) 14.7 us of which 3.7 are what a call with next
+// to no keys takes; 148 heads x 16384 keys (640 MB) 157 us, 4.1 TB/s; the kernel with tiles took 29.7 for the former.  A step of 16 keys is
+// 580 instructions of a warp, 2.4 us with 16 warps an SM (128 registers): it waits for its next codes (2.4 of 7.5 cycles an
+// issue) and for dependent instructions (1.5), the ALU pipe is busy for half of the time.  Steps three ahead in shared
+// memory by cp.async: 212 instead of 155 us, as what they cost in instructions is more than the wait.  The maximum of every
+// step by shuffles: 155 instead of 151.  16 queries a warp: 241 registers, one block an SM, slower than tiles from 9 queries on.
 #include <cuda_bf16.h>
 
 #include "attn_sched.h"
@@ -38,9 +45,16 @@ struct FewParams {
   int32_t run_row0[kMaxStreamsPerLaunch][3], run_end[kMaxStreamsPerLaunch][3];   // rows of the runs, added up
 };
 
+struct Yes {
+  __device__ constexpr operator bool() const { return true; }
+};
+struct No {
+  __device__ constexpr operator bool() const { return false; }
+};
+
 // D (16 x 8) += A (16 x 16) B (16 x 8)
 __device__ __forceinline__ void mma16816(float* d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
@@ -177,11 +191,12 @@ window_attn_few_kernel(const __grid_constant__ FewParams p, const uint4* q_rot, 
 #pragma unroll 1
   for (; step < hi; step += kFewWarps) {
     float s[4] = {0.f, 0.f, 0.f, 0.f};
-    // one factor up to a scale byte of 134, else 2^120 and another
-    const bool two_k = __any_sync(0xFFFFFFFFu, max(ek[0], ek[1]) > 134u);
-    {
-      uint32_t f[2] = {factor_small(ek[0]), factor_small(ek[1])};
-      if (__builtin_expect(two_k, 0)) f[0] = q8::factor1(ek[0]), f[1] = q8::factor1(ek[1]);
+    // One factor up to a scale byte of 134, else 2^120 and another: two loops, as a branch in the one would keep the compiler
+    // from interleaving its turns.
+    auto scores = [&](auto two) {
+      uint32_t f[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) f[i] = two ? q8::factor1(ek[i]) : factor_small(ek[i]);
 #pragma unroll
       for (int w = 0; w < 8; ++w) {
         uint2 y[2];
@@ -190,14 +205,16 @@ window_attn_few_kernel(const __grid_constant__ FewParams p, const uint4* q_rot, 
           y[i] = spread_pairs(xk[i][w]);
           y[i].x = q8::mul_bf16x2(y[i].x, f[i]);
           y[i].y = q8::mul_bf16x2(y[i].y, f[i]);
-          if (__builtin_expect(two_k, 0)) {
+          if (two) {
             y[i].x = q8::mul_bf16x2(y[i].x, q8::factor2(ek[i]));
             y[i].y = q8::mul_bf16x2(y[i].y, q8::factor2(ek[i]));
           }
         }
         mma16816(s, y[0].x, y[1].x, y[0].y, y[1].y, q[2 * w], q[2 * w + 1]);
       }
-    }
+    };
+    if (__builtin_expect(__any_sync(0xFFFFFFFFu, max(ek[0], ek[1]) > 134u), 0)) scores(Yes{});
+    else scores(No{});
     const int next = step + kFewWarps;
     if (next < hi) load_k(next);
     const int left = keys - step * kFewKeys;   // keys of this step
@@ -238,12 +255,15 @@ window_attn_few_kernel(const __grid_constant__ FewParams p, const uint4* q_rot, 
     }
     // P is rounded to bf16, as the operand that the matrix product takes
     const uint32_t pt0 = transpose8x8(pack_bf16x2(s[0], s[1])), pt1 = transpose8x8(pack_bf16x2(s[2], s[3]));
-    const bool two_v = __any_sync(0xFFFFFFFFu, max(max(ev[0], ev[1]), max(ev[2], ev[3])) > 134u);
-    {
+    auto values = [&](auto two) {
       // factors of the two keys of a pair side by side
-      uint32_t f[2] = {__byte_perm(factor_small(ev[0]), factor_small(ev[1]), 0x5410), __byte_perm(factor_small(ev[2]), factor_small(ev[3]), 0x5410)};
-      if (__builtin_expect(two_v, 0))
-        f[0] = __byte_perm(q8::factor1(ev[0]), q8::factor1(ev[1]), 0x5410), f[1] = __byte_perm(q8::factor1(ev[2]), q8::factor1(ev[3]), 0x5410);
+      uint32_t f[2], f2[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t e0 = ev[2 * i], e1 = ev[2 * i + 1];
+        f[i] = two ? __byte_perm(q8::factor1(e0), q8::factor1(e1), 0x5410) : __byte_perm(factor_small(e0), factor_small(e1), 0x5410);
+        f2[i] = two ? __byte_perm(q8::factor2(e0), q8::factor2(e1), 0x5410) : 0u;
+      }
 #pragma unroll
       for (int w = 0; w < 8; ++w) {   // two of the thread's 16 dims
         uint2 y[2];
@@ -255,15 +275,16 @@ window_attn_few_kernel(const __grid_constant__ FewParams p, const uint4* q_rot, 
           y[i] = spread_pairs(__byte_perm(wa, wd, (w & 1) ? 0x7632 : 0x5410));
           y[i].x = q8::mul_bf16x2(y[i].x, f[i]);
           y[i].y = q8::mul_bf16x2(y[i].y, f[i]);
-          if (__builtin_expect(two_v, 0)) {
-            const uint32_t f2 = __byte_perm(q8::factor2(ev[2 * i]), q8::factor2(ev[2 * i + 1]), 0x5410);
-            y[i].x = q8::mul_bf16x2(y[i].x, f2);
-            y[i].y = q8::mul_bf16x2(y[i].y, f2);
+          if (two) {
+            y[i].x = q8::mul_bf16x2(y[i].x, f2[i]);
+            y[i].y = q8::mul_bf16x2(y[i].y, f2[i]);
           }
         }
         mma16816(o[w], y[0].x, y[0].y, y[1].x, y[1].y, pt0, pt1);
       }
-    }
+    };
+    if (__builtin_expect(__any_sync(0xFFFFFFFFu, max(max(ev[0], ev[1]), max(ev[2], ev[3])) > 134u), 0)) values(Yes{});
+    else values(No{});
     if (next < hi) load_v(next);
   }
 

@@ -1,5 +1,6 @@
 // 8-bit cache: e4m3 codes, a power of two (e8m0 byte) for every 32 neighbouring dims.  Device code shared by
-// the append, the read and the attention.
+// the append, the read and the attention.  A power of two, and not a float: codes times it are exact in bf16 (4 significant
+// bits of 8), so that whoever decodes, into registers, a tile or memory, gets the same operand and rounds nothing.
 #pragma once
 
 #include <cuda_bf16.h>

@@ -97,8 +97,10 @@ __device__ __forceinline__ int partner_lane(const RotaryPlace& p, int lane, int 
 }
 
 // --------------------------------------------------------------------------
-// Rotation of one tensor.  A thread has the same place of up to kApplyHeads heads of a token: it fetches
-// its coefficients once, and its loads are in flight together.
+// Rotation of one tensor, HBM bound.  A thread has the same place of up to kApplyHeads heads of a token: it fetches
+// its coefficients once, and its loads are in flight together.  Halves: the two halves of a pair are 8 vectors or less
+// apart, in the same 16 lanes, and meet by a shuffle, so that every element is read once and in place works.  40
+// heads x 10800 tokens, halves of the first 96 dims (225 MB): 37.2 us, 6.06 TB/s, 0.92 of the measured copy rate.
 // --------------------------------------------------------------------------
 constexpr int kApplyHeads = 4;
 
@@ -154,6 +156,13 @@ rotary_apply_kernel(const ApplyParams p, const uint4* x_in, const float4* cos_t,
 // Append into the 8-bit cache.  `width` threads have a token: a thread the same place of kU heads in q, k and v, `width`
 // vectors apart (kWide: more than that, kU at a time); a block has one token with the norm, whose sum meets in shared memory, else
 // `tokens` of them.  Four neighbouring threads hold a block of 32 dims and find its largest magnitude with two shuffles.
+//
+// HBM bound without the norm: four streams of 4680 tokens x 12 heads (299 MB) 51.5 us, 5.8 TB/s, 0.88 of the measured copy rate;
+// three heads a thread 55.5, two 58, four 62, one 71 (with the same inputs each time, before the 64-bit division by the
+// number of threads of a token was taken out, which gave 51.2 -> 49.7).  With the norm a block's chain bounds it (loads, sum over
+// the block, gains, rotation, conversion; 4.7 long-scoreboard stalls an issue): one stream (75 MB) 20.1 us, 3.7 TB/s.  There
+// 10 blocks of 96 threads an SM 20.3, 8 21.3, 11 and 12 (spills) 22.6, 192 threads 22.9, 64 21.9; without the gains 16.0; the
+// table's row in registers from the start, as without the norm, 22.3; v behind the sum 22.9.
 // --------------------------------------------------------------------------
 struct Append8Params {
   RotaryPlace place;
@@ -351,7 +360,8 @@ rotary_kv_append_q8_kernel(const Append8Params p, const uint4* q_in, const uint4
 }
 
 // --------------------------------------------------------------------------
-// Frames of the 8-bit cache as bf16.  A thread decodes 16 codes of k and of v; a block stays in one frame.
+// Frames of the 8-bit cache as bf16, HBM bound.  A thread decodes 16 codes of k and of v; a block stays in one frame, so
+// that nothing is divided.  12 frames of 3600 tokens x 40 heads (1.34 GB): 230 us, 5.8 TB/s, 0.89 of the measured copy rate.
 // --------------------------------------------------------------------------
 struct Read8Params {
   int32_t C, S, n_frames, frame0;      // frame0: first frame of this launch inside the read

@@ -225,6 +225,10 @@ ATTN = [
     ("sink_and_ring_wrapped", (2, 2, (8, 25), 3, 6, 3, 6, 2, (13, 6))),
     ("37_streams", (37, 1, (4, 10), 1, 4, 0, 4, 0, tuple(3 + b % 5 for b in range(37)))),
     ("clusters", (1, 8, (10, 32), 1, 17, 0, 17, 0, (20,))),
+    ("one_tile_many_items", (2, 90, (4, 30), 1, 9, 0, 9, 0, (20, 5))),
+    ("one_tile_shares", (1, 200, (1, 100), 1, 25, 0, 25, 0, (60,))),
+    ("one_tile_clusters", (1, 6, (1, 20), 1, 150, 1, 140, 1, (300,))),
+    ("768_queries", (1, 3, (3, 256), 1, 3, 0, 3, 0, (7,))),
     ("whole_and_parts", (1, 150, (5, 8), 4, 8, 0, 8, 0, (4,))),
     ("shares", (1, 80, (5, 8), 5, 64, 0, 64, 0, (59,))),
 ]
@@ -290,8 +294,9 @@ def test_few_queries_of_peaked_keys_in_rising_order():
     check(layer.attend([699], 700, 0, q), layer.attend_oracle([699], 700, 0, q), "rising")
 
 
-# From five pairs of query tiles on the window is unpacked first.
+# From four pairs of query tiles on the window is unpacked first.
 UNPACKED = [
+    ("769_queries", (1, 3, (1, 769), 1, 3, 0, 3, 0, (7,))),
     ("1025_queries", (1, 2, (5, 205), 1, 2, 0, 2, 0, (3,))),
     ("small_frames_wrapped", (2, 3, (7, 9), 20, 23, 1, 21, 1, (80, 20))),
     ("sink_and_ring_wrapped", (2, 2, (20, 21), 3, 6, 3, 6, 2, (13, 6))),
