@@ -11,12 +11,13 @@
 // others' parts, in part order, so the result does not depend on which one that is.  Streams of different length get
 // different numbers of blocks, which clusters could not have.
 //
-// Measured: one token each of three streams, 12 heads, 4096, 1235 and 4096 keys (30 MB) 14.7 us of which 3.7 are what a call with next
-// to no keys takes; 148 heads x 16384 keys (640 MB) 157 us, 4.1 TB/s; the kernel with tiles took 29.7 for the former.  A step of 16 keys is
-// 580 instructions of a warp, 2.4 us with 16 warps an SM (128 registers): it waits for its next codes (2.4 of 7.5 cycles an
-// issue) and for dependent instructions (1.5), the ALU pipe is busy for half of the time.  Steps three ahead in shared
-// memory by cp.async: 212 instead of 155 us, as what they cost in instructions is more than the wait.  The maximum of every
-// step by shuffles: 155 instead of 151.  16 queries a warp: 241 registers, one block an SM, slower than tiles from 9 queries on.
+// Measured: one token each of three streams, 12 heads, 4096, 1235 and 4096 keys (30 MB) 13.0 us, of which 3.4 are what a call with next
+// to no keys takes; 148 heads x 16384 keys (640 MB) 140 us, 4.6 TB/s; one head x 16384 keys 8.2 us.  The kernel with tiles took
+// 29.7 for the first.  Bound by the instructions of a step (16 keys, a warp; 16 warps an SM by 128 registers) and the
+// waits between them: 2.1 us, with the ALU pipe, which issues every other cycle, half busy.  The second of these cases with
+// steps three ahead in shared memory by cp.async 212 instead of 155 us (more instructions than wait), with the maximum of
+// every step by shuffles 155 instead of 151, with the branch for the second factor inside the loops 157 instead of 140, with two
+// sums for S 142.  16 queries a warp: 241 registers, one block an SM, slower than tiles from 9 queries on.
 #include <cuda_bf16.h>
 
 #include "attn_sched.h"
@@ -30,7 +31,7 @@ using namespace ptx;
 
 constexpr int kFewWarps = 8, kFewThreads = 32 * kFewWarps;
 constexpr int kFewKeys = 16;                    // keys of a warp's step
-constexpr int kFewParts = 64;                   // most blocks of an item
+constexpr int kFewParts = 64;                   // most blocks of an item: two for each lane of a warp that merges them
 constexpr float kFewJump = 57.f;                // as far (log2) a score may be above the reference, as in attn.cu
 
 struct FewParams {
@@ -372,16 +373,27 @@ window_attn_few_kernel(const __grid_constant__ FewParams p, const uint4* q_rot, 
   const int64_t part0 = block - part;
   const int shares = p.L <= 1 ? 8 : p.L <= 2 ? 4 : p.L <= 4 ? 2 : 1, query = warp / shares, share = warp - query * shares;
   if (query < p.L) {
-    float all = -INFINITY, sum = 0.f;
-#pragma unroll 4
-    for (int k = share; k < parts; k += shares) all = fmaxf(all, __ldcg(part2 + (part0 + k) * kPart2 + kMl2 + query).x);
+    // Lane j looks up the references of the j-th and the (j + 32)-th part of this warp; then all lanes add part by part.
+    const int mine = (parts - share + shares - 1) / shares;
+    float2 ml[2];
+    float all = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int k = share + shares * (lane + 32 * i);
+      ml[i] = k < parts ? __ldcg(part2 + (part0 + k) * kPart2 + kMl2 + query) : make_float2(-INFINITY, 0.f);
+      all = fmaxf(all, ml[i].x);
+    }
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) all = fmaxf(all, __shfl_xor_sync(0xFFFFFFFFu, all, d));
+    const float f0 = weight(ml[0].x, all), f1 = weight(ml[1].x, all);
+    float sum = fmaf(ml[0].y, f0, ml[1].y * f1);
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int k = share; k < parts; k += shares) {
-      const float2 ml = __ldcg(part2 + (part0 + k) * kPart2 + kMl2 + query);
-      const float f = weight(ml.x, all);
-      sum = fmaf(ml.y, f, sum);
-      add(acc, __ldcg(part4 + (part0 + k) * kPart4 + query * kCols + lane), f);
+#pragma unroll 8
+    for (int j = 0; j < mine; ++j) {
+      const float f = __shfl_sync(0xFFFFFFFFu, j < 32 ? f0 : f1, j & 31);
+      add(acc, __ldcg(part4 + (part0 + share + shares * j) * kPart4 + query * kCols + lane), f);
     }
     reinterpret_cast<float4*>(slab(share, query))[lane] = acc;
     if (lane == 0) slab_ml(share)[query] = make_float2(all, sum);

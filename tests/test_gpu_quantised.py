@@ -279,6 +279,60 @@ def test_attention_of_few_queries(name, v_power):
     assert U.poll_status() == 0
 
 
+def shifted(t: torch.Tensor, nbytes: int) -> torch.Tensor:
+    """A copy of t whose address is `nbytes` behind a multiple of 256."""
+    raw = torch.zeros(t.numel() * t.element_size() + 256 + nbytes, dtype=torch.uint8, device="cuda")
+    lo = -raw.data_ptr() % 256 + nbytes
+    out = raw[lo:lo + t.numel() * t.element_size()].view(t.dtype).view(t.shape)
+    out.view(torch.uint8).copy_(t.view(torch.uint8))
+    assert out.data_ptr() % 256 == nbytes
+    return out
+
+
+@pytest.mark.parametrize("tokens", [2, 30, 200, 900])             # each of the ways to attend
+def test_buffers_at_the_least_alignment(tokens):
+    # activations and codes on 16 bytes, scales on 4
+    sh = shape(1, 3, 1, 1, tokens, max(3, 300 // tokens))
+    layer = Layer(sh)
+    layer.fill(74)
+    q = layer.queries(75)
+    n = sh.ring_frames
+    want = layer.attend([n + 1], n, 0, q)
+    layer.cache_k, layer.cache_v = shifted(layer.cache_k, 16), shifted(layer.cache_v, 16)
+    layer.scale_k, layer.scale_v = shifted(layer.scale_k, 4), shifted(layer.scale_v, 4)
+    out = shifted(torch.full_like(q, float("nan")), 16)
+    U.window_attn_q8(layer.abi, 0, [n + 1], n, 0, shifted(q, 16), *layer.cache, out)
+    assert torch.equal(out.view(torch.int16), want.view(torch.int16))
+    back, moved = ([torch.empty((1, n, tokens, 3, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2)] for _ in range(2))
+    moved = [shifted(x, 16) for x in moved]
+    U.kv_read_q8(layer.abi, 0, [1], n, *layer.cache, *moved)
+    layer.upload()
+    U.kv_read_q8(layer.abi, 0, [1], n, *layer.cache, *back)
+    assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip(back, moved))
+    assert U.poll_status() == 0
+
+
+@pytest.mark.parametrize("tokens,heads", [(3, 40), (100, 12), (300, 12), (900, 6)])
+def test_calls_that_overlap_on_three_streams(tokens, heads):
+    # each stream has a scratch of its own: parts, counters and unpacked windows
+    layers = []
+    for i in range(3):
+        layer = Layer(shape(1, heads, 1, 1, tokens, 2500 // tokens + 1))
+        layer.fill_codes(80 + i)
+        layers.append((layer, layer.queries(85 + i)))
+    n = layers[0][0].sh.ring_frames
+    want = [layer.attend([n], n, 0, q) for layer, q in layers]
+    streams, outs = [torch.cuda.Stream() for _ in range(3)], [torch.empty_like(q) for _, q in layers]
+    torch.cuda.synchronize()
+    for _ in range(8):
+        for (layer, q), st, o in zip(layers, streams, outs):
+            U.window_attn_q8(layer.abi, 0, [n], n, 0, q, *layer.cache, o, stream=st)
+    torch.cuda.synchronize()
+    for a, b in zip(want, outs):
+        assert torch.equal(a.view(torch.int16), b.view(torch.int16))
+    assert U.poll_status() == 0
+
+
 def test_few_queries_of_peaked_keys_in_rising_order():
     # every step of a warp has a larger maximum than the one before: sums and results are rescaled each time
     sh = shape(1, 2, 1, 1, 2, 700)
