@@ -299,16 +299,21 @@ int unstep_kv_read_q8(const unstep_shape_t* shape, int32_t sink_frames, const in
 /*
  * unstep_window_attn_sink over such a cache: the same frames, the same softmax, the keys and values as they are read back.
  *   q_rot, out : bf16 [B, L, Hn, 128].
- * Scratch: that of unstep_window_attn, shared with it; all it says about streams, captures and graphs holds here.  A call with
- * more than 768 queries a stream also unpacks the windows, as many heads at a time as fit, into a buffer of 16 to
- * 256 MB per stream, made by the first call that needs that size and kept until unstep_shutdown (smaller ones of former
- * calls are kept too, for graphs).  Where it cannot be made - no memory left, or inside a capture - the call decodes
- * as it goes, which takes up to a third longer; a result may then differ in its last bits.  Calls of up to 8
- * queries a stream read the cache without tiles.
+ * Scratch: that of unstep_window_attn, shared with it; all it says about streams, captures and graphs holds here.  Where windows
+ * are unpacked in front of the attention (more than 768 queries a stream, but for the smallest calls), as many heads at a time
+ * as fit, that goes into a buffer of 16 to 256 MB per stream, made by the first call that needs that size and kept until
+ * unstep_shutdown (smaller ones of former calls are kept too, for graphs).  Where it cannot be made - no memory left, or
+ * inside a capture - the call decodes as it goes, which takes up to a third longer; a result may then differ in its last bits.
+ *
+ * unstep_window_attn_q8_way says how such a call is run on a device of `max_workers` SMs (unstep_attn_workers): *way (HOST) is 0
+ * where keys go straight from the cache to the products (few queries, or few keys), 1 where tiles are decoded in the attention
+ * kernel, 2 where windows are unpacked in front of it.  Host only, no GPU is needed: a diagnostic for tests and tuning.
  */
 int unstep_window_attn_q8(const unstep_shape_t* shape, int32_t sink_frames, const int32_t* start_frame,
                           int32_t recent_frames, int32_t sink_attend, const void* q_rot, const void* cache_k,
                           const void* scale_k, const void* cache_v, const void* scale_v, void* out, void* cuda_stream);
+int unstep_window_attn_q8_way(const unstep_shape_t* shape, int32_t sink_frames, const int32_t* start_frame,
+                              int32_t recent_frames, int32_t sink_attend, int32_t max_workers, int32_t* way);
 
 /*
  * The work split of one unstep_window_attn(_sink) launch, listed on the host by the same integer

@@ -21,6 +21,7 @@ from .binding import (  # noqa: F401
     rotary_kv_append_q8,
     kv_read_q8,
     window_attn_q8,
+    window_attn_q8_way,
     window_attn_plan,
     attn_workers,
     attn_clusters,

@@ -16,8 +16,8 @@ EXPORTS = ("unstep_rope_table", "unstep_rope_kv_append", "unstep_window_attn",
            "unstep_window_attn_noalloc", "unstep_rope_kv_append_sink", "unstep_window_attn_sink",
            "unstep_rmsnorm_rope_kv_append", "unstep_window_attn_plan", "unstep_window_attn_plan_clusters",
            "unstep_rotary_table", "unstep_rotary_apply", "unstep_rotary_kv_append_q8", "unstep_kv_read_q8",
-           "unstep_window_attn_q8", "unstep_attn_workers", "unstep_attn_clusters", "unstep_selftest_wait_limit",
-           "unstep_shutdown", "unstep_strerror", "unstep_poll_status", "unstep_launch_count")
+           "unstep_window_attn_q8", "unstep_window_attn_q8_way", "unstep_attn_workers", "unstep_attn_clusters",
+           "unstep_selftest_wait_limit", "unstep_shutdown", "unstep_strerror", "unstep_poll_status", "unstep_launch_count")
 
 
 class UnstepError(RuntimeError):
@@ -123,6 +123,9 @@ def lib() -> ctypes.CDLL:
         L.unstep_window_attn_q8.restype = c_int
         L.unstep_window_attn_q8.argtypes = [POINTER(Shape), c_int32, POINTER(c_int32), c_int32, c_int32] + \
             [c_void_p] * 7
+        L.unstep_window_attn_q8_way.restype = c_int
+        L.unstep_window_attn_q8_way.argtypes = [POINTER(Shape), c_int32, POINTER(c_int32), c_int32, c_int32, c_int32,
+                                                POINTER(c_int32)]
         L.unstep_attn_clusters.restype = c_int
         L.unstep_attn_clusters.argtypes = [POINTER(c_int32)]
         L.unstep_attn_workers.restype = c_int
@@ -523,6 +526,17 @@ def _general_window_attn_q8(shape, sink_frames, start_frame, recent_frames, sink
         ctypes.byref(shape), int(sink_frames), _starts(shape, start_frame), int(recent_frames), int(sink_attend),
         _here_ptr(q_rot, bf, n, "q_rot"), *_cache8_ptrs(shape, sink_frames, cache_k, scale_k, cache_v, scale_v),
         _here_ptr(out, bf, n, "out"), _stream_ptr(stream)), "unstep_window_attn_q8")
+
+
+def window_attn_q8_way(shape: Shape, sink_frames: int, start_frame, recent_frames: int, sink_attend: int,
+                       max_workers: int) -> str:
+    """unstep_window_attn_q8_way: how window_attn_q8 is run on a device of max_workers SMs: "few", "tiles" or
+    "unpacked".  Host only."""
+    way = c_int32(-1)
+    _check(lib().unstep_window_attn_q8_way(ctypes.byref(shape), int(sink_frames), _starts(shape, start_frame),
+                                           int(recent_frames), int(sink_attend), int(max_workers), ctypes.byref(way)),
+           "unstep_window_attn_q8_way")
+    return ("few", "tiles", "unpacked")[way.value]
 
 
 def window_attn_plan(shape: Shape, start_frame, recent_frames: int, max_workers: int, sink_frames: int = 0,

@@ -73,3 +73,15 @@ extern "C" int unstep_window_attn_plan(const unstep_shape_t* shape, int32_t sink
   return unstep_window_attn_plan_clusters(shape, sink_frames, start_frame, recent_frames, sink_attend, max_workers,
                                           nullptr, segs, max_segs, n_segs);
 }
+
+extern "C" int unstep_window_attn_q8_way(const unstep_shape_t* shape, int32_t sink_frames, const int32_t* start_frame,
+                                         int32_t recent_frames, int32_t sink_attend, int32_t max_workers, int32_t* way) {
+  using namespace unstep;
+  const int rc = check_attn_args(shape, start_frame, recent_frames, sink_frames, sink_attend, true);
+  if (rc != UNSTEP_OK) return rc;
+  if (max_workers < 1 || max_workers > 65536 || way == nullptr) return UNSTEP_ERR_INVALID_ARG;
+  AttnParams p;
+  plan_shape(p, shape, sink_frames);
+  *way = q8_way(p, shape, start_frame, recent_frames, sink_attend, max_workers);
+  return UNSTEP_OK;
+}

@@ -1107,7 +1107,6 @@ struct DeviceInfo {
   bool ok = false;
   int sm_count = 0;
   int32_t clusters[kKinds][kMaxClusterParts + 1] = {};   // clusters of that many blocks which the device runs at the same time
-  int32_t few_blocks = 0;   // blocks of the kernel for few queries that an SM holds
 };
 
 template <Kind kKind>
@@ -1143,7 +1142,7 @@ static DeviceInfo query_device(int dev) {
   DeviceInfo info;
   info.ok = cudaDeviceGetAttribute(&info.sm_count, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess &&
             query_kernels<kBf16>(info.clusters[kBf16]) &&
-            query_kernels<kQ8Pairs>(info.clusters[kQ8Pairs]) && query_kernels<kQ8Lone>(info.clusters[kQ8Lone]) && few_setup(&info.few_blocks);
+            query_kernels<kQ8Pairs>(info.clusters[kQ8Pairs]) && query_kernels<kQ8Lone>(info.clusters[kQ8Lone]);
   if (!info.ok) return info;
   return known[dev] = info;
 }
@@ -1424,13 +1423,6 @@ extern "C" int unstep_window_attn_sink(const unstep_shape_t* shape, int32_t sink
                          get_workspace, sink_frames, sink_attend);
 }
 
-// Query-tile pairs of a head from which on the window of an 8-bit cache is unpacked in front of the attention.  Unpacking moves
-// 5 bytes a dim through DRAM whatever the queries; decoding tiles takes each query pair of a head 0.5 to 1 us a key tile.  us,
-// decoded in the kernel / unpacked: 2 pairs, 24 heads x 4000 keys 40.2 / 42.7, x 16000 108 / 125; 4 pairs, x 800 22.4 / 20.2, x
-// 4000 71.4 / 66.1, x 16000 208 / 197; 5 pairs, x 3600 81.9 / 61.7; 19 pairs, 12 heads x 32760 951 / 741.  Of few items (2 heads) the
-// two are within 5 % of each other.
-constexpr int kUnpackPairs = 4;
-
 // Attention over an 8-bit cache with few queries, or with many, by way of unpacked windows, as many heads at a time as the
 // scratch holds.  Leaves `done` false where the kernel that decodes tiles for itself is to do it.  With many queries every
 // tile of a head is decoded once here, and by each query pair of the head there, next to a softmax that needs the issue slots.
@@ -1442,7 +1434,6 @@ static int window_attn_q8_run(const unstep_shape_t* shape, int32_t sink_frames, 
   if (rc != UNSTEP_OK) return rc;
   AttnParams p;
   plan_shape(p, shape, sink_frames);
-  if (p.L > kFewQueries && p.q_pairs < kUnpackPairs) return UNSTEP_OK;
   const void* ptrs[] = {q_rot, cache_k, cache_v, out};
   for (const void* ptr : ptrs)
     if (ptr == nullptr || !aligned16(ptr)) return UNSTEP_ERR_INVALID_ARG;
@@ -1455,15 +1446,16 @@ static int window_attn_q8_run(const unstep_shape_t* shape, int32_t sink_frames, 
   const int64_t row_bytes = Hn * kHeadDim * 2;
   p.flat = p.padded = 1;
   p.cache_rows = cache_rows;
-  if (p.L <= kFewQueries) {
+  const Way way = q8_way(p, shape, start_frame, window_frames, sink_attend, info.sm_count);
+  if (way == kFew) {
     for (int64_t b0 = 0; b0 < shape->batch; b0 += kMaxStreamsPerLaunch) {
       const int nb = static_cast<int>(shape->batch - b0 < kMaxStreamsPerLaunch ? shape->batch - b0 : kMaxStreamsPerLaunch);
       plan_windows(p, shape, start_frame + b0, nb, window_frames, sink_frames, sink_attend);
-      p.items_per_stream = p.Hn;
+      p.items_per_stream = p.Hn * few_groups(p.L);
       rc = bind_scratch(p, st, get_workspace, info.sm_count, out, 0);
       if (rc != UNSTEP_OK) return rc;
       const int64_t act = b0 * L * row_bytes, rows = b0 * cache_rows * Hn;
-      rc = launch_few(p, nb, info.sm_count, info.few_blocks, static_cast<const char*>(q_rot) + act, static_cast<const char*>(cache_k) + rows * kHeadDim,
+      rc = launch_few(p, nb, info.sm_count, static_cast<const char*>(q_rot) + act, static_cast<const char*>(cache_k) + rows * kHeadDim,
                       static_cast<const char*>(scale_k) + rows * 4, static_cast<const char*>(cache_v) + rows * kHeadDim,
                       static_cast<const char*>(scale_v) + rows * 4, static_cast<char*>(out) + act, st);
       if (rc != UNSTEP_OK) return rc;
@@ -1471,6 +1463,7 @@ static int window_attn_q8_run(const unstep_shape_t* shape, int32_t sink_frames, 
     *done = true;
     return UNSTEP_OK;
   }
+  if (way == kTiles) return UNSTEP_OK;
   // the widest window decides how many streams and heads go together
   int64_t rows = 0;
   for (int b = 0; b < shape->batch; ++b) {

@@ -1,4 +1,5 @@
-// Attention of at most 8 queries a stream over an 8-bit cache (sm_100a): single tokens, and what little more goes with them.
+// Attention of few queries, or over few keys, of an 8-bit cache (sm_100a): single tokens, and launches that would be over
+// before the kernel with tiles has its first one done.
 //
 // DRAM bound: every cached key and value is read once, and a query tile of the tensor-memory kernel would be next to empty,
 // while it waits for tiles to be decoded into shared memory.  Here a warp takes 16 keys at a time straight from global memory
@@ -7,7 +8,7 @@
 // The dims of K, summed over, and those of V, independent of each other, may come in any order, so every thread
 // reads 16 or 32 neighbouring codes of a row and needs no exchange; P^T turns from result to operand by a
 // transpose of its 8 x 8 blocks.  Each warp has its own running maximum and sum; the warps of a block merge through
-// shared memory, the blocks of an item (stream, head) through the scratch: the one that is done last reads the
+// shared memory, the blocks of an item (stream, head, 8 queries) through the scratch: the one that is done last reads the
 // others' parts, in part order, so the result does not depend on which one that is.  Streams of different length get
 // different numbers of blocks, which clusters could not have.
 //
@@ -17,7 +18,8 @@
 // waits between them: 2.1 us, with the ALU pipe, which issues every other cycle, half busy.  The second of these cases with
 // steps three ahead in shared memory by cp.async 212 instead of 155 us (more instructions than wait), with the maximum of
 // every step by shuffles 155 instead of 151, with the branch for the second factor inside the loops 157 instead of 140, with two
-// sums for S 142.  16 queries a warp: 241 registers, one block an SM, slower than tiles from 9 queries on.
+// sums for S 142.  16 queries a warp, which would read keys half as often: 241 registers, one block an SM, slower than tiles
+// from 9 queries on; groups of 8 find the keys in L2.
 #include <cuda_bf16.h>
 
 #include "attn_sched.h"
@@ -29,13 +31,12 @@ namespace unstep {
 
 using namespace ptx;
 
-constexpr int kFewWarps = 8, kFewThreads = 32 * kFewWarps;
-constexpr int kFewKeys = 16;                    // keys of a warp's step
+constexpr int kFewThreads = 32 * kFewWarps;
 constexpr int kFewParts = 64;                   // most blocks of an item: two for each lane of a warp that merges them
 constexpr float kFewJump = 57.f;                // as far (log2) a score may be above the reference, as in attn.cu
 
 struct FewParams {
-  int32_t Hn, L, n_streams;
+  int32_t Hn, L, groups, n_streams;             // groups of kFewQueries queries
   int64_t cache_rows;                           // rows of a stream's cache
   float scale_log2e;
   float* part;                                  // scratch: part_floats for every block
@@ -79,7 +80,7 @@ constexpr int kFewPartFloats = kFewQueries * kHeadDim + kFewQueries * 2;
 
 // kWide: cache_k is 32-byte aligned.
 template <bool kWide>
-__global__ void __launch_bounds__(kFewThreads, 2)
+__global__ void __launch_bounds__(kFewThreads, kFewBlocks)
 window_attn_few_kernel(const __grid_constant__ FewParams p, const uint4* q_rot, const uint4* cache_k, const uint8_t* scale_k,
                        const uint4* cache_v, const uint8_t* scale_v, uint32_t* out) {
   __shared__ __align__(16) uint8_t few_smem[kFewWarps * kFewWarpBytes];
@@ -91,7 +92,8 @@ window_attn_few_kernel(const __grid_constant__ FewParams p, const uint4* q_rot, 
   const int block = static_cast<int>(blockIdx.x);
   int b = 0;
   while (b + 1 < p.n_streams && p.block0[b + 1] <= block) ++b;
-  const int parts = p.parts[b], h = (block - p.block0[b]) / parts, part = block - p.block0[b] - h * parts;
+  const int parts = p.parts[b], item = (block - p.block0[b]) / parts, part = block - p.block0[b] - item * parts;
+  const int h = item / p.groups, query0 = kFewQueries * (item - h * p.groups), queries = min(kFewQueries, p.L - query0);
   const int end0 = p.run_end[b][0], end1 = p.run_end[b][1], keys = p.run_end[b][2];
   const int row0 = p.run_row0[b][0], row1 = p.run_row0[b][1] - end0, row2 = p.run_row0[b][2] - end1;
   const int steps = (keys + kFewKeys - 1) / kFewKeys;
@@ -109,7 +111,7 @@ window_attn_few_kernel(const __grid_constant__ FewParams p, const uint4* q_rot, 
   const uint4* const head_v = cache_v + head * 8;
   const uint8_t* const head_ek = scale_k + head * 4;
   const uint8_t* const head_ev = scale_v + head * 4;
-  const uint4* const head_q = q_rot + (b * (static_cast<int64_t>(p.L) - p.cache_rows) * p.Hn + head) * 16;
+  const uint4* const head_q = q_rot + ((b * (static_cast<int64_t>(p.L) - p.cache_rows) + query0) * p.Hn + head) * 16;
   const uint32_t row_codes = 8u * p.Hn, row_scales = 4u * p.Hn;
 
   // B of S^T: thread (g, c) has query g, dims 32 c .. in pairs (0, 2) and (1, 3) of four, as spread_pairs makes them
@@ -117,7 +119,7 @@ window_attn_few_kernel(const __grid_constant__ FewParams p, const uint4* q_rot, 
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     uint4 x = make_uint4(0, 0, 0, 0);
-    if (g < p.L) x = __ldca(head_q + static_cast<int64_t>(g) * p.Hn * 16 + 4 * c + i);
+    if (g < queries) x = __ldca(head_q + static_cast<int64_t>(g) * p.Hn * 16 + 4 * c + i);
     q[4 * i] = __byte_perm(x.x, x.y, 0x5410), q[4 * i + 1] = __byte_perm(x.x, x.y, 0x7632);
     q[4 * i + 2] = __byte_perm(x.z, x.w, 0x5410), q[4 * i + 3] = __byte_perm(x.z, x.w, 0x7632);
   }
@@ -296,7 +298,7 @@ window_attn_few_kernel(const __grid_constant__ FewParams p, const uint4* q_rot, 
     for (int d = 4; d < 32; d <<= 1) l[e] += __shfl_xor_sync(0xFFFFFFFFu, l[e], d);
     const int query = 2 * c + e;
     if (g == 0) slab_ml(warp)[query] = make_float2(m[e], l[e]);
-    if (query < p.L) {
+    if (query < queries) {
       float* const to = slab(warp, query) + 16 * g;
 #pragma unroll
       for (int t = 0; t < 8; ++t) *reinterpret_cast<float2*>(to + 2 * t) = make_float2(o[t][e], o[t][2 + e]);
@@ -312,7 +314,7 @@ window_attn_few_kernel(const __grid_constant__ FewParams p, const uint4* q_rot, 
     acc.w = fmaf(x.w, f, acc.w);
   };
   auto store = [&](int query, int col, float4 acc, float inv) {
-    const int64_t dst = (((static_cast<int64_t>(b) * p.L + query) * p.Hn + h) * kHeadDim + 4 * col) / 2;
+    const int64_t dst = (((static_cast<int64_t>(b) * p.L + query0 + query) * p.Hn + h) * kHeadDim + 4 * col) / 2;
     UNSTEP_STORE(out, dst, p.extent_out, pack_bf16x2(acc.x * inv, acc.y * inv), p.status);
     UNSTEP_STORE(out, dst + 1, p.extent_out, pack_bf16x2(acc.z * inv, acc.w * inv), p.status);
   };
@@ -322,7 +324,7 @@ window_attn_few_kernel(const __grid_constant__ FewParams p, const uint4* q_rot, 
   constexpr int kPart4 = kFewPartFloats / 4, kMl2 = kFewQueries * kHeadDim / 2, kPart2 = kFewPartFloats / 2;
   // the first `slabs` results in shared memory as one, to the scratch or to the result
   auto merge_slabs = [&](int slabs, bool to_scratch) {
-    for (int i = threadIdx.x; i < p.L * kCols; i += kFewThreads) {
+    for (int i = threadIdx.x; i < queries * kCols; i += kFewThreads) {
       const int query = i / kCols, col = i - query * kCols;
       float all = -INFINITY, sum = 0.f;
       float2 ml[kFewWarps];
@@ -351,7 +353,7 @@ window_attn_few_kernel(const __grid_constant__ FewParams p, const uint4* q_rot, 
   merge_slabs(kFewWarps, parts > 1);
   if (parts == 1) return;
   // ---- blocks of the item ----
-  const int64_t counter = static_cast<int64_t>(b) * p.Hn + h;
+  const int64_t counter = static_cast<int64_t>(b) * p.Hn * p.groups + item;
   __syncthreads();   // all of this part is stored, and shared memory is free
   if (threadIdx.x == 0) {
     int before = -1;
@@ -371,8 +373,8 @@ window_attn_few_kernel(const __grid_constant__ FewParams p, const uint4* q_rot, 
   // A warp has a query (the warps that are left over share the parts of one), a lane four dims of it, and what the
   // warps of a query have is merged as above.
   const int64_t part0 = block - part;
-  const int shares = p.L <= 1 ? 8 : p.L <= 2 ? 4 : p.L <= 4 ? 2 : 1, query = warp / shares, share = warp - query * shares;
-  if (query < p.L) {
+  const int shares = queries <= 1 ? 8 : queries <= 2 ? 4 : queries <= 4 ? 2 : 1, query = warp / shares, share = warp - query * shares;
+  if (query < queries) {
     // Lane j looks up the references of the j-th and the (j + 32)-th part of this warp; then all lanes add part by part.
     const int mine = (parts - share + shares - 1) / shares;
     float2 ml[2];
@@ -402,18 +404,12 @@ window_attn_few_kernel(const __grid_constant__ FewParams p, const uint4* q_rot, 
   merge_slabs(shares, false);
 }
 
-bool few_setup(int32_t* blocks_per_sm) {
-  int n = 0;
-  if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, window_attn_few_kernel<true>, kFewThreads, 0) != cudaSuccess) return false;
-  *blocks_per_sm = n;
-  return n > 0;
-}
-
-int launch_few(const AttnParams& a, int nb, int sm_count, int32_t blocks_per_sm, const void* q_rot, const void* cache_k,
-               const void* scale_k, const void* cache_v, const void* scale_v, void* out, cudaStream_t st) {
+int launch_few(const AttnParams& a, int nb, int sm_count, const void* q_rot, const void* cache_k, const void* scale_k,
+               const void* cache_v, const void* scale_v, void* out, cudaStream_t st) {
   FewParams p;
   p.Hn = a.Hn;
   p.L = a.L;
+  p.groups = few_groups(a.L);
   p.n_streams = nb;
   p.cache_rows = a.cache_rows;
   p.scale_log2e = a.scale_log2e;
@@ -431,11 +427,11 @@ int launch_few(const AttnParams& a, int nb, int sm_count, int32_t blocks_per_sm,
       p.run_end[i][r] = end += a.run_rows[i][r];
     }
     steps[i] = (end + kFewKeys - 1) / kFewKeys;
-    all += steps[i] * a.Hn;
+    all += steps[i] * a.Hn * p.groups;
   }
   // The shortest share of steps for a block with which all blocks run at once (a second wave would take as long as
   // the first), but at least one for each of its warps; with more items than blocks an item is not split.
-  const int64_t room = static_cast<int64_t>(sm_count) * blocks_per_sm;
+  const int64_t room = static_cast<int64_t>(sm_count) * kFewBlocks;
   const int64_t part_room = p.extent_part / kFewPartFloats;
   int64_t share = (all + room - 1) / room, blocks = 0;
   if (share < kFewWarps) share = kFewWarps;
@@ -448,7 +444,7 @@ int launch_few(const AttnParams& a, int nb, int sm_count, int32_t blocks_per_sm,
       const int64_t parts = (steps[i] + share - 1) / share;
       p.parts[i] = static_cast<int32_t>(parts);
       p.block0[i] = static_cast<int32_t>(blocks);
-      blocks += parts * a.Hn;
+      blocks += parts * a.Hn * p.groups;
       split = split || parts > 1;
     }
     if (!split || (blocks <= room && blocks <= part_room)) break;

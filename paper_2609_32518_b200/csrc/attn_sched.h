@@ -417,12 +417,62 @@ inline void plan_shape(AttnParams& p, const unstep_shape_t* shape, int32_t sink_
   p.cache_rows = 0;
 }
 
-// The kernel for launches of at most kFewQueries queries a stream over an 8-bit cache (attn_few.cu): how many of its blocks
-// an SM of the current device holds, and a launch over the windows and with the scratch of `a`.  Host only.
-constexpr int kFewQueries = 8;
-bool few_setup(int32_t* blocks_per_sm);
-int launch_few(const AttnParams& a, int nb, int sm_count, int32_t blocks_per_sm, const void* q_rot, const void* cache_k,
-               const void* scale_k, const void* cache_v, const void* scale_v, void* out, cudaStream_t st);
+// The kernel for few queries or keys of an 8-bit cache (attn_few.cu), which takes kFewQueries of a stream at a time, and a
+// launch of it over the windows and with the scratch of `a`.
+constexpr int kFewQueries = 8, kFewKeys = 16, kFewWarps = 8;   // queries of an item, keys of a step, warps of a block
+constexpr int kFewBlocks = 2;                                  // blocks that an SM holds
+inline int32_t few_groups(int32_t L) { return (L + kFewQueries - 1) / kFewQueries; }
+int launch_few(const AttnParams& a, int nb, int sm_count, const void* q_rot, const void* cache_k, const void* scale_k,
+               const void* cache_v, const void* scale_v, void* out, cudaStream_t st);
+
+// Query-tile pairs of a head from which on the window of an 8-bit cache is unpacked in front of the attention.  Unpacking moves
+// 5 bytes a dim through DRAM whatever the queries; decoding tiles takes each query pair of a head 0.5 to 1 us a key tile.  us,
+// decoded in the kernel / unpacked: 2 pairs, 24 heads x 4000 keys 40.2 / 42.7, x 16000 108 / 125; 4 pairs, x 800 22.4 / 20.2, x
+// 4000 71.4 / 66.1, x 16000 208 / 197; 5 pairs, x 3600 81.9 / 61.7; 19 pairs, 12 heads x 32760 951 / 741.  Of few items (2 heads) the
+// two are within 5 % of each other.
+constexpr int kUnpackPairs = 4;
+
+// Whether the kernel without tiles is estimated to be shorter.  A turn of its blocks is a step of 16 keys for each of
+// their warps, whatever the queries (one group of 8 or less); a key tile is a step of a thread block with tiles.  The
+// estimates (us) are fitted to launches of 1 to 120 heads, 9 to 660 queries and 40 to 5300 keys.  Measured, us, with tiles / without: 2 heads x
+// 21 queries x 511 keys 10.2 / 7.3, 9 x 42 x 98 8.3 / 3.9, 6 x 30 x 1320 21.7 / 9.2, 1 x 312 x 5304 24.8 / 18.4, 5 x 201 x 1139
+// 15.4 / 14.4; and 15 x 40 x 1600 13.3 / 14.5, 30 x 80 x 320 11.5 / 12.3, 36 x 75 x 100 8.5 / 9.1, 31 x 189 x 630 15.9 / 34.1.  A single group
+// is never slower: 12 heads x 4 queries x 256 keys 9.9 / 7.5, 40 x 4 x 32000 154 / 89.
+inline bool few_is_shorter(const AttnParams& p, const unstep_shape_t* shape, const int32_t* start_frame, int32_t window_frames,
+                           int32_t sink_attend, int32_t sm_count) {
+  const int64_t groups = few_groups(p.L);
+  if (groups == 1) return true;
+  const int64_t nb = shape->batch < kMaxStreamsPerLaunch ? shape->batch : kMaxStreamsPerLaunch;   // of one launch
+  const int64_t room = static_cast<int64_t>(sm_count) * kFewBlocks, items = nb * p.Hn * groups;
+  if (items > 64 * room) return false;   // 2.3 us a turn of two groups or more against 1.4 of a tile that serves them all
+  int64_t all = 0, most = 0;   // keys
+  for (int b = 0; b < nb; ++b) {
+    const int64_t hi = static_cast<int64_t>(start_frame[b]) + shape->chunk_frames, lo = hi > window_frames ? hi - window_frames : 0;
+    const int64_t keys = ((sink_attend < lo ? sink_attend : lo) + hi - lo) * p.T;
+    all += keys;
+    most = keys > most ? keys : most;
+  }
+  const int64_t steps = all / kFewKeys * p.Hn * groups, longest = (most + kFewKeys - 1) / kFewKeys;
+  int64_t share = (steps + room - 1) / room;
+  if (share < kFewWarps) share = kFewWarps;
+  if (share > longest) share = longest;
+  const int64_t waves = share < longest ? 1 : (items + room - 1) / room;
+  const double without = 4.5 + 2.3 * static_cast<double>(waves * ((share + kFewWarps - 1) / kFewWarps));
+  const int64_t pairs = nb * p.Hn * p.q_pairs, tiles = (most + kTileN - 1) / kTileN;
+  const int64_t parts = sm_count / pairs < 1 ? 1 : (sm_count / pairs < kMaxClusterParts ? sm_count / pairs : kMaxClusterParts);
+  const double step = p.q_tiles == 1 || p.q_pairs >= kUnpackPairs ? 1.4 : 2.4;
+  const double with = 7.0 + (parts > 1 && tiles > 1 ? 2.5 : 0.0) + (p.q_pairs >= kUnpackPairs ? 4.0 : 0.0) +
+                      step * static_cast<double>((pairs + sm_count - 1) / sm_count * ((tiles + parts - 1) / parts));
+  return without < with;
+}
+
+// The way in which a call over an 8-bit cache is run (its first launch decides).
+enum Way { kFew, kTiles, kUnpacked };
+inline Way q8_way(const AttnParams& p, const unstep_shape_t* shape, const int32_t* start_frame, int32_t window_frames,
+                  int32_t sink_attend, int32_t sm_count) {
+  if (few_is_shorter(p, shape, start_frame, window_frames, sink_attend, sm_count)) return kFew;
+  return p.q_pairs < kUnpackPairs ? kTiles : kUnpacked;
+}
 
 // Argument checks shared by the attention entry points and the plan entry point (no device needed).
 inline int check_attn_args(const unstep_shape_t* shape, const int32_t* start_frame, int32_t window_frames,

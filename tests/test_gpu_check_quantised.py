@@ -97,6 +97,8 @@ def _child():
     run("token", shape(1, 1, 1, 1, 1, 5), 0, [7], 5, 0, 128, False)
     run("ragged", shape(2, 3, 3, 8, 25, 7), 0, [12, 3], 7, 0, 128, True)
     run("sink", shape(2, 5, 2, 3, 7, 9), 2, [21, 8], 8, 1, 96, True)
+    run("sink, many heads", shape(2, 40, 2, 3, 7, 9), 2, [21, 8], 8, 1, 96, True)
+    run("groups", shape(1, 2, 1, 7, 13, 6), 0, [9], 6, 0, 128, True)
     run("37 streams", shape(37, 1, 1, 4, 10, 4), 0, [3 + b % 5 for b in range(37)], 4, 0, 16, False)
     run("norm", shape(2, 12, 1, 3, 11, 4), 1, [5, 9], 4, 1, 128, True, norm=True)
     run("wide norm", shape(1, 70, 1, 1, 9, 3), 0, [4], 3, 0, 64, False, norm=True)

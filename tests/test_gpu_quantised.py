@@ -210,6 +210,12 @@ def check(got: torch.Tensor, ref, what):
     assert mx <= MAX_ABS and mean <= MEAN_ABS and rel <= REL_L2, f"{what}: {mx:.3e} {mean:.3e} {rel:.3e}"
 
 
+def assert_way(layer: Layer, want: str, starts, recent, attend=0):
+    """A call on so many streams, heads, queries and keys reaches the kernel that its test is about."""
+    way = U.window_attn_q8_way(layer.abi, layer.sink, starts, recent, attend, U.attn_workers()[0])
+    assert way == want, f"{way} instead of {want}"
+
+
 ATTN = [
     # batch, heads, grid, chunk, ring, sink, recent, sink_attend, starts
     ("one_key", (1, 1, (1, 1), 1, 1, 0, 1, 0, (0,))),
@@ -224,6 +230,14 @@ ATTN = [
     ("ragged", (2, 3, (8, 25), 3, 7, 0, 5, 0, (12, 3))),
     ("sink_and_ring_wrapped", (2, 2, (8, 25), 3, 6, 3, 6, 2, (13, 6))),
     ("37_streams", (37, 1, (4, 10), 1, 4, 0, 4, 0, tuple(3 + b % 5 for b in range(37)))),
+    ("17_queries_33_keys_many_heads", (1, 200, (1, 17), 1, 2, 0, 2, 0, (50,))),
+    ("127_keys_many_heads", (1, 20, (1, 127), 1, 1, 0, 1, 0, (4,))),
+    ("128_keys_many_heads", (1, 20, (8, 16), 1, 1, 0, 1, 0, (4,))),
+    ("129_keys_many_heads", (1, 20, (3, 43), 1, 1, 0, 1, 0, (4,))),
+    ("short_frames_wrapped_many_heads", (2, 20, (5, 7), 2, 9, 1, 7, 1, (31, 8))),
+    ("first_chunk_many_heads", (1, 12, (8, 25), 3, 7, 3, 7, 3, (0,))),
+    ("37_streams_many_heads", (37, 12, (4, 10), 1, 4, 0, 4, 0, tuple(3 + b % 5 for b in range(37)))),
+    ("one_tile_clusters_many_heads", (1, 20, (1, 20), 1, 150, 1, 140, 1, (300,))),
     ("clusters", (1, 8, (10, 32), 1, 17, 0, 17, 0, (20,))),
     ("one_tile_many_items", (2, 90, (4, 30), 1, 9, 0, 9, 0, (20, 5))),
     ("one_tile_shares", (1, 200, (1, 100), 1, 25, 0, 25, 0, (60,))),
@@ -232,6 +246,8 @@ ATTN = [
     ("whole_and_parts", (1, 150, (5, 8), 4, 8, 0, 8, 0, (4,))),
     ("shares", (1, 80, (5, 8), 5, 64, 0, 64, 0, (59,))),
 ]
+TILES = ("ragged", "sink_and_ring_wrapped", "clusters", "one_tile_many_items", "one_tile_shares", "768_queries",
+         "whole_and_parts", "shares")
 
 
 @pytest.mark.parametrize("name", [n for n, _ in ATTN])
@@ -239,6 +255,7 @@ def test_attention(name):
     batch, heads, grid, fc, ring, sink, recent, attend, starts = dict(ATTN)[name]
     sh = shape(batch, heads, fc, *grid, ring)
     layer = Layer(sh, sink)
+    assert_way(layer, "tiles" if name in TILES or name.endswith("many_heads") else "few", starts, recent, attend)
     layer.fill(20, k_scale=2.0)
     q = layer.queries(21)
     some = sorted({0, heads // 2, heads - 1})
@@ -249,7 +266,7 @@ def test_attention(name):
         q = q.flip(1).contiguous()
 
 
-# Up to 8 queries a stream: keys go straight from memory into warp-level products.
+# Few queries, or few keys: keys go straight from memory into warp-level products, for 8 queries at a time.
 FEW = [
     ("8_queries_one_key", (1, 1, (1, 8), 1, 1, 0, 1, 0, (0,))),
     ("9_queries", (2, 3, (3, 3), 1, 40, 2, 33, 1, (100, 7))),
@@ -259,7 +276,13 @@ FEW = [
     ("34_streams", (34, 3, (1, 2), 1, 90, 1, 70, 1, tuple(3 * b for b in range(34)))),
     ("long", (1, 1, (1, 1), 1, 9001, 0, 9001, 0, (20000,))),
     ("many_items", (3, 40, (1, 1), 1, 200, 0, 200, 0, (300, 10, 199))),
-    ("no_scratch_queries_17", (1, 2, (1, 17), 1, 9, 0, 9, 0, (20,))),
+    ("17_queries", (1, 2, (1, 17), 1, 9, 0, 9, 0, (20,))),
+    ("33_queries_one_frame", (3, 2, (3, 11), 1, 2, 0, 1, 0, (0, 7, 1))),
+    ("63_queries_wrapped", (2, 3, (3, 7), 3, 19, 2, 16, 2, (40, 3))),
+    ("100_queries_whole_items", (1, 5, (10, 10), 1, 1, 0, 1, 0, (6,))),
+    ("303_queries_parts", (1, 1, (3, 101), 1, 11, 0, 11, 0, (30,))),
+    ("35_streams_of_10_queries", (35, 1, (2, 5), 1, 30, 1, 27, 1, tuple(2 * b for b in range(35)))),
+    ("801_queries", (1, 1, (9, 89), 1, 1, 0, 1, 0, (2,))),
 ]
 
 
@@ -269,6 +292,7 @@ def test_attention_of_few_queries(name, v_power):
     batch, heads, grid, fc, ring, sink, recent, attend, starts = dict(FEW)[name]
     sh = shape(batch, heads, fc, *grid, ring)
     layer = Layer(sh, sink)
+    assert_way(layer, "few", starts, recent, attend)
     layer.fill(70, k_scale=2.0, v_power=v_power)
     q = layer.queries(71)
     got, ref = layer.attend(starts, recent, attend, q), layer.attend_oracle(starts, recent, attend, q)
@@ -289,11 +313,13 @@ def shifted(t: torch.Tensor, nbytes: int) -> torch.Tensor:
     return out
 
 
-@pytest.mark.parametrize("tokens", [2, 30, 200, 900])             # each of the ways to attend
-def test_buffers_at_the_least_alignment(tokens):
+@pytest.mark.parametrize("tokens,heads,way", [(2, 3, "few"), (30, 3, "few"), (30, 90, "tiles"), (200, 20, "tiles"),
+                                               (900, 3, "unpacked")])
+def test_buffers_at_the_least_alignment(tokens, heads, way):
     # activations and codes on 16 bytes, scales on 4
-    sh = shape(1, 3, 1, 1, tokens, max(3, 300 // tokens))
+    sh = shape(1, heads, 1, 1, tokens, max(3, 300 // tokens))
     layer = Layer(sh)
+    assert_way(layer, way, [sh.ring_frames + 1], sh.ring_frames)
     layer.fill(74)
     q = layer.queries(75)
     n = sh.ring_frames
@@ -303,7 +329,7 @@ def test_buffers_at_the_least_alignment(tokens):
     out = shifted(torch.full_like(q, float("nan")), 16)
     U.window_attn_q8(layer.abi, 0, [n + 1], n, 0, shifted(q, 16), *layer.cache, out)
     assert torch.equal(out.view(torch.int16), want.view(torch.int16))
-    back, moved = ([torch.empty((1, n, tokens, 3, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2)] for _ in range(2))
+    back, moved = ([torch.empty((1, n, tokens, heads, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2)] for _ in range(2))
     moved = [shifted(x, 16) for x in moved]
     U.kv_read_q8(layer.abi, 0, [1], n, *layer.cache, *moved)
     layer.upload()
@@ -312,8 +338,9 @@ def test_buffers_at_the_least_alignment(tokens):
     assert U.poll_status() == 0
 
 
-@pytest.mark.parametrize("tokens,heads", [(3, 40), (100, 12), (300, 12), (900, 6)])
-def test_calls_that_overlap_on_three_streams(tokens, heads):
+@pytest.mark.parametrize("tokens,heads,way", [(3, 40, "few"), (25, 3, "few"), (100, 12, "tiles"), (300, 12, "tiles"),
+                                               (900, 6, "unpacked")])
+def test_calls_that_overlap_on_three_streams(tokens, heads, way):
     # each stream has a scratch of its own: parts, counters and unpacked windows
     layers = []
     for i in range(3):
@@ -321,6 +348,7 @@ def test_calls_that_overlap_on_three_streams(tokens, heads):
         layer.fill_codes(80 + i)
         layers.append((layer, layer.queries(85 + i)))
     n = layers[0][0].sh.ring_frames
+    assert_way(layers[0][0], way, [n], n)
     want = [layer.attend([n], n, 0, q) for layer, q in layers]
     streams, outs = [torch.cuda.Stream() for _ in range(3)], [torch.empty_like(q) for _, q in layers]
     torch.cuda.synchronize()
@@ -333,19 +361,21 @@ def test_calls_that_overlap_on_three_streams(tokens, heads):
     assert U.poll_status() == 0
 
 
-def test_few_queries_of_peaked_keys_in_rising_order():
+@pytest.mark.parametrize("tokens,frames", [(2, 700), (28, 50)])
+def test_few_queries_of_peaked_keys_in_rising_order(tokens, frames):
     # every step of a warp has a larger maximum than the one before: sums and results are rescaled each time
-    sh = shape(1, 2, 1, 1, 2, 700)
+    sh = shape(1, 2, 1, 1, tokens, frames)
     layer = Layer(sh)
     rng = np.random.default_rng(72)
     k = rng.standard_normal(layer.ora.cache_k.shape).astype(np.float32)
-    k[..., 0] = np.linspace(0, 200, 700, dtype=np.float32)[None, :, None, None]
+    k[..., 0] = np.linspace(0, 200, frames, dtype=np.float32)[None, :, None, None]
     layer.ora.cache_k, layer.ora.scale_k = Q.quantise(k)
     layer.ora.cache_v, layer.ora.scale_v = Q.quantise(rng.standard_normal(k.shape).astype(np.float32))
     layer.upload()
     q = layer.queries(73)
     q[..., 0] = 3.0
-    check(layer.attend([699], 700, 0, q), layer.attend_oracle([699], 700, 0, q), "rising")
+    assert_way(layer, "few", [frames - 1], frames)
+    check(layer.attend([frames - 1], frames, 0, q), layer.attend_oracle([frames - 1], frames, 0, q), "rising")
 
 
 # From four pairs of query tiles on the window is unpacked first.
@@ -364,6 +394,7 @@ def test_attention_over_unpacked_windows(name):
     batch, heads, grid, fc, ring, sink, recent, attend, starts = dict(UNPACKED)[name]
     sh = shape(batch, heads, fc, *grid, ring)
     layer = Layer(sh, sink)
+    assert_way(layer, "unpacked", starts, recent, attend)
     layer.fill_codes(50)
     q = layer.queries(51)
     rows = W.sample_rows(sh.chunk_tokens)
@@ -415,9 +446,11 @@ def test_unpacked_window_of_a_captured_graph_survives_larger_calls():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out.view(torch.int16), want.view(torch.int16))
+    assert_way(small, "unpacked", [4], 2)
     # a capture on a stream that has no scratch yet decodes inside the attention, within the bounds
     fresh, other = torch.cuda.Stream(), torch.zeros_like(q)
-    few = Layer(shape(1, 2, 1, 4, 10, 2))
+    few = Layer(shape(1, 60, 1, 4, 10, 2))
+    assert_way(few, "tiles", [4], 2)
     few.fill_codes(59)
     q_few = few.queries(60)
     torch.cuda.synchronize()
@@ -431,12 +464,14 @@ def test_unpacked_window_of_a_captured_graph_survives_larger_calls():
     assert U.poll_status() == 0
 
 
-def test_attention_leaves_what_it_does_not_attend_alone():
+@pytest.mark.parametrize("heads,way", [(2, "few"), (12, "tiles")])
+def test_attention_leaves_what_it_does_not_attend_alone(heads, way):
     # every slot outside the window holds NaN blocks, and codes that nobody writes
-    sh = shape(2, 2, 2, 3, 19, 8)
+    sh = shape(2, heads, 2, 3, 19, 8)
     layer = Layer(sh, 2)
     layer.fill(30)
     starts, recent, attend = (9, 15), 5, 1
+    assert_way(layer, way, starts, recent, attend)
     for b, s in enumerate(starts):
         frames = O.sink_window_frames(s, 2, recent, attend)
         held = {O.sink_slot(p, 2, 8) for p in frames}
@@ -448,26 +483,31 @@ def test_attention_leaves_what_it_does_not_attend_alone():
     check(layer.attend(starts, recent, attend, q), layer.attend_oracle(starts, recent, attend, q), "poisoned")
 
 
-def test_attention_over_a_nan_block_is_nan_for_its_head_only():
-    sh = shape(1, 2, 1, 8, 20, 3)
+@pytest.mark.parametrize("heads,way", [(2, "few"), (12, "tiles")])
+def test_attention_over_a_nan_block_is_nan_for_its_head_only(heads, way):
+    sh = shape(1, heads, 1, 8, 20, 3)
     layer = Layer(sh)
+    assert_way(layer, way, [2], 3)
     layer.fill(32)
     layer.ora.scale_v[0, 1, 77, 1, 2] = 255
     layer.upload()
     q = layer.queries(33)
     got, ref = layer.attend([2], 3, 0, q), layer.attend_oracle([2], 3, 0, q)
     nan = np.isnan(ref)
-    assert nan[:, :, 1, 64:96].all() and not nan[:, :, 0].any() and nan.sum() == 160 * 32
+    assert nan[:, :, 1, 64:96].all() and nan.sum() == 160 * 32
     assert np.array_equal(np.isnan(got.float().cpu().numpy()), nan)
-    check(got[:, :, :1], ref[:, :, :1], "the other head")
+    others = [h for h in range(heads) if h != 1]
+    check(got[:, :, others], ref[:, :, others], "the other heads")
 
 
+@pytest.mark.parametrize("heads,way", [(2, "few"), (12, "tiles")])
 @pytest.mark.parametrize("power", [-100, -40, 20, 60, 100])
-def test_attention_with_values_far_from_one(power):
+def test_attention_with_values_far_from_one(power, heads, way):
     # scale bytes above 134 take a second factor; the result is the one of values near 1, scaled: 2^-11 of the unscaled
     # relative error is lost nowhere
-    sh = shape(1, 2, 1, 7, 23, 3)
+    sh = shape(1, heads, 1, 7, 23, 3)
     layer = Layer(sh)
+    assert_way(layer, way, [2], 3)
     layer.fill(34, v_power=power)
     q = layer.queries(35)
     got = layer.attend([2], 3, 0, q).double().cpu().numpy()
@@ -476,9 +516,11 @@ def test_attention_with_values_far_from_one(power):
     assert np.linalg.norm((got - ref) * 2.0 ** -power) <= REL_L2 * np.linalg.norm(ref * 2.0 ** -power)
 
 
-def test_attention_with_peaked_scores():
-    sh = shape(1, 2, 2, 8, 25, 6)
+@pytest.mark.parametrize("heads,way", [(2, "few"), (3, "tiles")])
+def test_attention_with_peaked_scores(heads, way):
+    sh = shape(1, heads, 2, 8, 25, 6)
     layer = Layer(sh)
+    assert_way(layer, way, [9], 6)
     layer.fill(36, k_scale=40.0)
     q = layer.queries(37)
     check(layer.attend([9], 6, 0, q), layer.attend_oracle([9], 6, 0, q), "peaked")

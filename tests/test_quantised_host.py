@@ -197,3 +197,33 @@ def test_runs_of_the_cache_are_those_of_a_walk_over_the_frames():
             prev = slot + 1
         segs = U.window_attn_plan(sh, [start], window, 148, sink, attend)
         assert segs[0][7] == sum((r + 127) // 128 for r in runs), (tokens, sink, ring, window, start, attend)
+
+
+def test_way_of_a_call():
+    def way(batch, heads, queries, keys, workers=148, **kw):
+        # one frame of `queries` tokens, keys / queries of them in the window
+        n = keys // queries
+        sh = U.Shape.make(batch, heads, 1, 1, queries, n, **kw)
+        return U.window_attn_q8_way(sh, 0, [n + 5] * batch, n, 0, workers)
+
+    assert {way(b, h, q, k) for b in (1, 40) for h in (1, 4096) for q in (1, 8) for k in (8, 800)} == {"few"}
+    assert way(1, 2, 100, 300) == "few" and way(1, 40, 100, 300) == "tiles" and way(1, 2, 100, 300, 4) == "tiles"
+    assert way(1, 2, 768, 1 << 20) == "tiles" and way(1, 2, 769, 769 << 10) == "unpacked"
+    # the largest that the checks let through: 2^30 cache rows less one frame of them, all heads, all streams
+    assert way(1 << 20, 2, 1 << 20, 1023 << 20) == "unpacked"
+    assert way(1 << 20, 4096, 1 << 15, 16 << 15, 65536) == "unpacked" and way(1, 4096, 1 << 19, 1 << 19, 1) == "unpacked"
+
+
+def test_way_of_a_call_refuses():
+    def way(shape=good_shape(), sink=0, first=(0, 2), recent=2, attend=0, workers=148, out=True):
+        got = ctypes.c_int32(7)
+        rc = U.lib().unstep_window_attn_q8_way(ctypes.byref(shape), sink, starts(first), recent, attend, workers,
+                                               ctypes.byref(got) if out else None)
+        assert rc == 0 or got.value == 7
+        return rc
+
+    assert way() == 0
+    for kw in (dict(sink=-1), dict(first=None), dict(first=(0, -1)), dict(recent=1), dict(recent=7), dict(attend=1),
+               dict(workers=0), dict(workers=65537), dict(out=False), dict(shape=good_shape(batch=0))):
+        assert way(**kw) == INVALID, kw
+    assert way(shape=good_shape(head_dim=64)) == UNSUPPORTED
