@@ -223,7 +223,7 @@ int unstep_window_attn_noalloc(const unstep_shape_t* shape, const int32_t* start
  *
  * R = band_t + band_h + band_w of the shape, a multiple of 16 from 16 to 128, is the rotated part of a head; dims
  * R .. 127 pass through.  In the calls that take an unstep_rope_t, and in those on a quantised cache, a band may be 0
- * (one axis only: band_t = R on a grid of 1 x T).  Pair j in [0, R/2) is (x[2j], x[2j+1]), with `half` (x[j], x[j + R/2]).  Its
+ * (text has one axis: band_t = R, a frame for each token, a grid of 1 x 1).  Pair j in [0, R/2) is (x[2j], x[2j+1]), with `half` (x[j], x[j + R/2]).  Its
  * frequency, for local pair i of the band of axis a with d_a dims, is
  *     omega = rope_base^(-2i/d_a)
  *     omega' = omega * (keep + (1 - keep) / factor[a]),   keep = clamp((trained[a] * omega / (2 pi) - beta_slow)

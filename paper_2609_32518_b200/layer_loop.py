@@ -95,6 +95,9 @@ class ChunkStepper:
         two bf16 tensors [B, n_frames, T, Hn, 128].  The frames must still be held."""
         import torch
         sh = self.shape
+        if first_frame < 0 or n_frames < 1 or first_frame + n_frames - max(first_frame, self.sink) > sh.ring_frames:
+            raise ValueError(f"frames [{first_frame}, {first_frame + n_frames}): no run that {self.sink} sink frames and a "
+                             f"ring of {sh.ring_frames} hold at once")
         if self.quantised:
             out = [torch.empty((sh.batch, n_frames, sh.tokens_per_frame, sh.heads, sh.head_dim), dtype=torch.bfloat16,
                                device=self.device) for _ in range(2)]

@@ -68,6 +68,16 @@ def test_read_frames_of_a_bf16_cache_are_its_slots():
         ChunkStepper(make(sh), 1, 3, rope=U.Rope.make(half=True))
 
 
+@pytest.mark.parametrize("quantised", [False, True])
+def test_read_frames_refuses_what_no_cache_holds(quantised):
+    sh = W.Shape(batch=1, heads=2, chunk_frames=1, grid_h=2, grid_w=3, ring_frames=3)
+    stepper = ChunkStepper(make(sh), 1, 3, 1, 1, quantised=quantised)
+    for first, n in ((-1, 2), (0, 0), (0, 5), (2, 4)):
+        with pytest.raises(ValueError, match="hold at once"):
+            stepper.read_frames(0, first, n)
+    assert stepper.read_frames(0, 0, 4)[0].shape == (1, 4, 6, 2, 128)    # the sink frame and three of the ring
+
+
 @pytest.mark.parametrize("grid", [(8, 8), (20, 20)])   # a window decoded in the attention, and one unpacked for it
 def test_graph_of_a_chunk_replays_what_the_calls_do(grid):
     sh = W.Shape(batch=1, heads=4, chunk_frames=2, grid_h=grid[0], grid_w=grid[1], ring_frames=6)
