@@ -162,7 +162,10 @@ rotary_apply_kernel(const ApplyParams p, const uint4* x_in, const float4* cos_t,
 // number of threads of a token was taken out, which gave 51.2 -> 49.7).  With the norm a block's chain bounds it (loads, sum over
 // the block, gains, rotation, conversion; 4.7 long-scoreboard stalls an issue): one stream (75 MB) 20.1 us, 3.7 TB/s.  There
 // 10 blocks of 96 threads an SM 20.3, 8 21.3, 11 and 12 (spills) 22.6, 192 threads 22.9, 64 21.9; without the gains 16.0; the
-// table's row in registers from the start, as without the norm, 22.3; v behind the sum 22.9.
+// table's row in registers from the start, as without the norm, 22.3; v behind the sum 22.9.  Gains brought to shared memory
+// meanwhile: 19.3, but interleaved 18.4 instead of 17.8 and 10800 tokens 42.5 instead of 41.4; blocks that go through the
+// tokens with the next one's vectors on their way 34.  With four heads a thread at least two blocks an SM (128
+// registers) for interleaved pairs, 40 heads 61.1 -> 54.5, 48 82.8 -> 65.7, and not for halves, which then spill (64.6 -> 67.5).
 // --------------------------------------------------------------------------
 struct Append8Params {
   RotaryPlace place;
@@ -204,7 +207,7 @@ __device__ __forceinline__ void gain8(float* f, float r, const float4* gain, int
 }
 
 template <int kU, bool kHalf, bool kNorm, bool kWide>
-__global__ void __launch_bounds__(kNorm && kU <= 2 ? 96 : 256, kNorm && kU <= 2 ? 10 : 1)
+__global__ void __launch_bounds__(256, kNorm && kU <= 2 ? 4 : kNorm && !kHalf && !kWide ? 2 : 1)
 rotary_kv_append_q8_kernel(const Append8Params p, const uint4* q_in, const uint4* k_in, const uint4* v_in,
                            const float4* gain_q, const float4* gain_k, const float4* cos_t, const float4* sin_t,
                            uint4* q_out, uint2* cache_k, uint8_t* scale_k, uint2* cache_v, uint8_t* scale_v) {
@@ -475,7 +478,6 @@ static Append8Kernel append8_kernel(bool norm, int per_thread, bool wide) {
   switch (per_thread) {
     case 1: return rotary_kv_append_q8_kernel<1, kHalf, true, false>;
     case 2: return rotary_kv_append_q8_kernel<2, kHalf, true, false>;
-    case 3: return rotary_kv_append_q8_kernel<3, kHalf, true, false>;
     default: return rotary_kv_append_q8_kernel<4, kHalf, true, false>;
   }
 }
@@ -522,8 +524,10 @@ extern "C" int unstep_rotary_kv_append_q8(const unstep_shape_t* shape, const uns
   bool wide = false;
   int64_t blocks;
   if (norm) {
-    per_thread = (p.vec_per_token + 95) / 96;
-    if (per_thread > 4) per_thread = 4;
+    // Two heads a thread while a block has the threads: all loads of a token are in flight with 64 registers.  Halves /
+    // interleaved, 4680 tokens, us, two : three or four of them: 14 heads 24.5 / 20.9 : 27.9 / 26.2, 20 33.2 / 29.2 : 38.3 / 36.4,
+    // 32 49.2 / 42.7 : 51.4 / 47.6; with 36 in blocks of 288 threads 84.5 / 70.5 : 62.3 / 59.3.
+    per_thread = p.vec_per_token <= 96 ? 1 : p.vec_per_token <= 512 ? 2 : 4;
     threads = (((p.vec_per_token + per_thread - 1) / per_thread) + 31) & ~31;
     wide = threads > 256;
     if (wide) threads = 256;

@@ -175,7 +175,7 @@ def test_read_decodes_every_code_under_every_scale():
 
 
 @pytest.mark.parametrize("half", [False, True])
-@pytest.mark.parametrize("heads", [1, 5, 12, 40, 70])
+@pytest.mark.parametrize("heads", [1, 5, 6, 7, 12, 13, 17, 31, 32, 33, 40, 64, 70])   # both sides of each way to lay out a token
 def test_append_behind_the_norm(half, heads):
     sh = shape(2, heads, 1, 3, 5, 2)
     layer = Layer(sh, 0, Q.Rope(half=half), 96)
