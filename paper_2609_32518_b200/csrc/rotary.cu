@@ -157,9 +157,8 @@ rotary_apply_kernel(const ApplyParams p, const uint4* x_in, const float4* cos_t,
 // vectors apart (kWide: more than that, kU at a time); a block has one token with the norm, whose sum meets in shared memory, else
 // `tokens` of them.  Four neighbouring threads hold a block of 32 dims and find its largest magnitude with two shuffles.
 //
-// HBM bound without the norm: four streams of 4680 tokens x 12 heads (299 MB) 51.5 us, 5.8 TB/s, 0.88 of the measured copy rate;
-// three heads a thread 55.5, two 58, four 62, one 71 (with the same inputs each time, before the 64-bit division by the
-// number of threads of a token was taken out, which gave 51.2 -> 49.7).  With the norm a block's chain bounds it (loads, sum over
+// HBM bound without the norm: four streams of 4680 tokens x 12 heads (299 MB) 50.2 us, 6.0 TB/s, 0.91 of the measured copy rate.
+// With the norm a block's chain bounds it (loads, sum over
 // the block, gains, rotation, conversion; 4.7 long-scoreboard stalls an issue): one stream (75 MB) 20.1 us, 3.7 TB/s.  There
 // 10 blocks of 96 threads an SM 20.3, 8 21.3, 11 and 12 (spills) 22.6, 192 threads 22.9, 64 21.9; without the gains 16.0; the
 // table's row in registers from the start, as without the norm, 22.3; v behind the sum 22.9.  Gains brought to shared memory
@@ -468,7 +467,6 @@ static Append8Kernel append8_kernel(bool norm, int per_thread, bool wide) {
   if (!norm) {
     if (wide) return rotary_kv_append_q8_kernel<4, kHalf, false, true>;
     switch (per_thread) {
-      case 1: return rotary_kv_append_q8_kernel<1, kHalf, false, false>;
       case 2: return rotary_kv_append_q8_kernel<2, kHalf, false, false>;
       case 3: return rotary_kv_append_q8_kernel<3, kHalf, false, false>;
       default: return rotary_kv_append_q8_kernel<4, kHalf, false, false>;
@@ -535,12 +533,15 @@ extern "C" int unstep_rotary_kv_append_q8(const unstep_shape_t* shape, const uns
     p.tokens = 1;
     blocks = T;
   } else {
-    // three heads a thread, or the number of heads that leaves fewer of them without work
+    // Three heads a thread, or two (of few heads, four) where that leaves fewer threads without work; four where a block
+    // would not have the threads.  Halves / interleaved, 4680 tokens, us, one : two : three : four of them: 4 heads 5.8 / 5.0 :
+    // 5.7 / 4.3 : 6.6 / 5.8 : 4.6 / 4.3, 7 9.4 / 8.6 : 9.2 / 7.8 : 10.2 / 9.4 : 8.5 / 8.3, 12 16.4 / 15.4 : 15.7 / 14.6 : 15.1 / 14.6 :
+    // 17.8 / 17.7, 14 two 17.7 / 17.0, three 19.0 / 18.2, four 20.7 / 20.3, 20 24.8 / 22.6, 25.4 / 22.2 and 27.5 / 27.0.
     wide = shape->heads > 64;
-    per_thread = 3;
-    for (const int u : {4, 2, 1})
-      if ((shape->heads + u - 1) / u * u < (shape->heads + per_thread - 1) / per_thread * per_thread) per_thread = u;
-    if (wide || shape->heads > 16 * per_thread) per_thread = 4;
+    per_thread = shape->heads > 48 ? 4 : 3;
+    auto places = [&](int u) { return (shape->heads + u - 1) / u * u; };
+    if (shape->heads <= 8 && places(4) < places(per_thread)) per_thread = 4;
+    if (shape->heads <= 32 && places(2) < places(per_thread)) per_thread = 2;
     p.width = wide ? 256 : 16 * ((shape->heads + per_thread - 1) / per_thread);
     p.tokens = 256 / p.width;
     threads = (p.width * p.tokens + 31) & ~31;

@@ -113,7 +113,9 @@ def test_rotation_undone_by_its_transpose_and_gradient_by_differences():
 @pytest.mark.parametrize("half", [False, True])
 @pytest.mark.parametrize("rotated", [128, 96, 16])
 @pytest.mark.parametrize("batch,heads,grid,fc,ring,sink", [
-    (1, 1, (1, 1), 1, 3, 0), (2, 3, (3, 5), 2, 4, 1), (1, 12, (2, 9), 3, 3, 0), (35, 2, (1, 3), 1, 2, 2), (2, 17, (1, 7), 1, 2, 0)])
+    (1, 1, (1, 1), 1, 3, 0), (2, 3, (3, 5), 2, 4, 1), (1, 12, (2, 9), 3, 3, 0), (35, 2, (1, 3), 1, 2, 2), (2, 17, (1, 7), 1, 2, 0),
+    (1, 4, (1, 41), 1, 2, 0), (2, 7, (1, 19), 1, 2, 1), (1, 32, (1, 5), 1, 2, 0), (1, 33, (1, 3), 2, 3, 1), (2, 48, (1, 2), 1, 2, 0),
+    (1, 49, (1, 3), 1, 2, 1), (1, 65, (1, 3), 1, 2, 0)])
 def test_append_is_bit_exact_and_read_gives_it_back(half, rotated, batch, heads, grid, fc, ring, sink):
     sh = shape(batch, heads, fc, *grid, ring)
     layer = Layer(sh, sink, Q.Rope(half=half), rotated)
