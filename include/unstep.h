@@ -124,8 +124,8 @@ int unstep_rope_kv_append(const unstep_shape_t* shape, const int32_t* start_fram
  * Scratch: work items that are split across thread blocks exchange partial results through a
  * buffer the library keeps per (device, stream).  The first call on a stream creates it with
  * cudaMalloc (two slots per SM, about 40 MB, whatever the problem): make that call outside any stream
- * capture.  Calls on one stream share the buffer safely; calls on different streams use different
- * buffers.  Only the arrival counters depend on the problem: 8 bytes per work item (stream, head, pair
+ * capture.  Calls on one stream share the buffer safely, from whichever host threads they come; calls on
+ * different streams use different buffers.  Only the arrival counters depend on the problem: 8 bytes per work item (stream, head, pair
  * of 128-query tiles; up to 32 streams), independent of the start frames and the window.  The first
  * call of a stream with more than 2048 work items, and any later one with more than there is room
  * for, gets a larger array (again by cudaMalloc, outside any capture); the former one is kept, and
@@ -391,7 +391,8 @@ int unstep_selftest_wait_limit(int64_t limit_cycles, void* cuda_stream);
 
 /*
  * Optional: waits for the devices to go idle and frees the scratch buffers unstep_window_attn
- * created (all devices, all streams).  The library stays usable; the next call makes new ones.
+ * created (all devices, all streams).  No other call may be under way meanwhile, in another host thread.  The library
+ * stays usable; the next call makes new ones.
  */
 void unstep_shutdown(void);
 

@@ -1186,6 +1186,7 @@ struct StreamScratch {
   // unpacked windows of an 8-bit cache: the last one is in use, the smaller ones may be in captured graphs
   void* window[kWindowSizes] = {};
   int n_windows = 0;             // window[i] has kLeastWindow << i bytes, or is null
+  std::mutex window_turn;        // held by the call whose launches hand data on through a window (window_turn below)
 };
 static std::mutex g_ws_mutex;
 static std::map<std::pair<int, cudaStream_t>, StreamScratch> g_workspaces;
@@ -1222,7 +1223,21 @@ static int get_workspace(cudaStream_t st, size_t slots, size_t n_counters, Works
   return UNSTEP_OK;
 }
 
-// `bytes` (at most kMostWindow) for unpacked windows on this stream; null if there is no room, or if the stream
+// The turn of a call whose launches hand data on through the window buffer of this stream.  Stream order keeps one call's
+// launches from the next one's only if they are enqueued one behind the other, and another host thread may be in a call on the
+// same stream: so the turn is taken before the buffer is looked up and kept until the last launch that reads it is
+// enqueued.  (The calls that launch one kernel need none: it finds its scratch idle and leaves it so.)  g_ws_mutex is taken
+// for moments inside a turn, and never the other way round.
+static std::unique_lock<std::mutex> window_turn(cudaStream_t st) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return std::unique_lock<std::mutex>();   // get_window finds none then
+  std::unique_lock<std::mutex> lock(g_ws_mutex);
+  std::mutex& turn = g_workspaces[std::make_pair(dev, st)].window_turn;   // stays where it is until unstep_shutdown()
+  lock.unlock();
+  return std::unique_lock<std::mutex>(turn);
+}
+
+// `bytes` (at most kMostWindow) for unpacked windows on this stream, in the caller's turn; null if there is no room, or if the stream
 // is being captured and the buffer would have to be made.
 static void* get_window(cudaStream_t st, size_t bytes) {
   int dev = 0;
@@ -1478,6 +1493,7 @@ static int window_attn_q8_run(const unstep_shape_t* shape, int32_t sink_frames, 
   if (streams > room) streams = room;
   int64_t heads = room / streams < Hn ? room / streams : Hn;
   heads = (Hn + (Hn + heads - 1) / heads - 1) / ((Hn + heads - 1) / heads);   // groups of equal size
+  const std::unique_lock<std::mutex> turn = window_turn(st);   // to the end of the call
   uint8_t* const window = static_cast<uint8_t*>(get_window(st, streams * heads * per_head));
   if (window == nullptr) return UNSTEP_OK;
 
