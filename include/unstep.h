@@ -125,7 +125,7 @@ int unstep_rope_kv_append(const unstep_shape_t* shape, const int32_t* start_fram
  * buffer the library keeps per (device, stream).  The first call on a stream creates it with
  * cudaMalloc (two slots per SM, about 40 MB, whatever the problem): make that call outside any stream
  * capture.  Calls on one stream share the buffer safely, from whichever host threads they come; calls on
- * different streams use different buffers.  Only the arrival counters depend on the problem: 8 bytes per work item (stream, head, pair
+ * different streams use different buffers (cudaStreamPerThread is a stream of its own in every host thread).  Only the arrival counters depend on the problem: 8 bytes per work item (stream, head, pair
  * of 128-query tiles; up to 32 streams), independent of the start frames and the window.  The first
  * call of a stream with more than 2048 work items, and any later one with more than there is room
  * for, gets a larger array (again by cudaMalloc, outside any capture); the former one is kept, and

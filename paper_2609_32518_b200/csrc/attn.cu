@@ -31,9 +31,10 @@
 #include <cuda.h>
 #include <cuda_bf16.h>
 
+#include <atomic>
 #include <map>
 #include <mutex>
-#include <utility>
+#include <tuple>
 
 #include "common.h"
 #include "ptx.cuh"
@@ -1189,13 +1190,24 @@ struct StreamScratch {
   std::mutex window_turn;        // held by the call whose launches hand data on through a window (window_turn below)
 };
 static std::mutex g_ws_mutex;
-static std::map<std::pair<int, cudaStream_t>, StreamScratch> g_workspaces;
+// (device, stream, host thread): the handle cudaStreamPerThread means another stream in every host thread, so there the
+// thread counts too (by a number of its own: the system gives the id of a thread that has ended to another one, whose
+// stream could overlap what the ended one left under way); it is 0 with every other handle.
+typedef std::tuple<int, cudaStream_t, uint64_t> ScratchKey;
+static std::map<ScratchKey, StreamScratch> g_workspaces;
+static ScratchKey scratch_key(int dev, cudaStream_t st) {
+  static std::atomic<uint64_t> threads{0};
+  static thread_local uint64_t number = 0;
+  if (st != cudaStreamPerThread) return ScratchKey(dev, st, 0);
+  if (number == 0) number = ++threads;
+  return ScratchKey(dev, st, number);
+}
 
 static int get_workspace(cudaStream_t st, size_t slots, size_t n_counters, Workspace* out) {
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return UNSTEP_ERR_CUDA;
   std::lock_guard<std::mutex> lock(g_ws_mutex);
-  StreamScratch& s = g_workspaces[std::make_pair(dev, st)];
+  StreamScratch& s = g_workspaces[scratch_key(dev, st)];
   Workspace& ws = s.ws;
   if (ws.part == nullptr) {
     if (cudaMalloc(&ws.part, slots * kPartFloats * sizeof(float)) != cudaSuccess) {
@@ -1232,7 +1244,7 @@ static std::unique_lock<std::mutex> window_turn(cudaStream_t st) {
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return std::unique_lock<std::mutex>();   // get_window finds none then
   std::unique_lock<std::mutex> lock(g_ws_mutex);
-  std::mutex& turn = g_workspaces[std::make_pair(dev, st)].window_turn;   // stays where it is until unstep_shutdown()
+  std::mutex& turn = g_workspaces[scratch_key(dev, st)].window_turn;   // stays where it is until unstep_shutdown()
   lock.unlock();
   return std::unique_lock<std::mutex>(turn);
 }
@@ -1245,7 +1257,7 @@ static void* get_window(cudaStream_t st, size_t bytes) {
   int size = 0;
   while (kLeastWindow << size < bytes) ++size;
   std::lock_guard<std::mutex> lock(g_ws_mutex);
-  StreamScratch& s = g_workspaces[std::make_pair(dev, st)];
+  StreamScratch& s = g_workspaces[scratch_key(dev, st)];
   if (s.n_windows > size) return s.window[s.n_windows - 1];
   cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
   if (cudaStreamIsCapturing(st, &capture) != cudaSuccess || capture != cudaStreamCaptureStatusNone) {
@@ -1268,7 +1280,7 @@ static void reset_workspace_counters() {
   if (cudaGetDevice(&dev) != cudaSuccess) return;
   std::lock_guard<std::mutex> lock(g_ws_mutex);
   for (auto& kv : g_workspaces) {
-    if (kv.first.first != dev) continue;
+    if (std::get<0>(kv.first) != dev) continue;
     const StreamScratch& s = kv.second;
     if (s.ws.counters != nullptr) cudaMemset(s.ws.counters, 0, s.ws.n_counters * sizeof(int));
     for (int i = 0; i < s.n_left; ++i) cudaMemset(s.left[i].counters, 0, s.left[i].n_counters * sizeof(int));
@@ -1709,7 +1721,7 @@ extern "C" void unstep_shutdown(void) {
   if (cudaGetDevice(&cur) != cudaSuccess) return;
   std::lock_guard<std::mutex> lock(g_ws_mutex);
   for (auto& kv : g_workspaces) {
-    if (cudaSetDevice(kv.first.first) != cudaSuccess) continue;
+    if (cudaSetDevice(std::get<0>(kv.first)) != cudaSuccess) continue;
     cudaDeviceSynchronize();
     const StreamScratch& s = kv.second;
     if (s.ws.part != nullptr) cudaFree(s.ws.part);

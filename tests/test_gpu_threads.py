@@ -64,3 +64,43 @@ def test_two_threads_on_one_stream_with_unpacked_windows(heads, grid, frames, ca
         wrong = [i for i in range(calls) if not torch.equal(outs[i].view(torch.int16), want.view(torch.int16))]
         assert not wrong, f"{len(wrong)} of {calls} calls, the first is number {wrong[0]}"
     assert U.poll_status() == 0
+
+
+class PerThread:
+    """cudaStreamPerThread: one handle, a stream of its own in every host thread."""
+    cuda_stream = 2
+
+
+@pytest.mark.parametrize("quantised,tokens,heads,way", [(False, 200, 80, None), (True, 3, 40, "few"),
+                                                        (True, 300, 12, "tiles"), (True, 900, 6, "unpacked")])
+def test_the_per_thread_streams_of_two_threads_have_a_scratch_each(quantised, tokens, heads, way):
+    work, calls, n = [], 60, 2500 // tokens + 1
+    for seed in range(2):
+        layer = Layer(W.Shape(batch=1, heads=heads, chunk_frames=1, grid_h=1, grid_w=tokens, ring_frames=n))
+        layer.fill_codes(60 + seed)
+        if quantised:
+            assert U.window_attn_q8_way(layer.abi, 0, [n], n, 0, U.attn_workers()[0]) == way
+            call = lambda q, o, st, x=layer: U.window_attn_q8(x.abi, 0, [n], n, 0, q, *x.cache, o, stream=st)
+        else:
+            ring = [torch.empty((1, n, tokens, heads, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+            U.kv_read_q8(layer.abi, 0, [0], n, *layer.cache, *ring)
+            call = lambda q, o, st, x=layer, r=ring: U.window_attn(x.abi, [n - 1], n, q, *r, o, stream=st)
+            # parts that are merged through the scratch
+            plan = U.window_attn_plan(layer.abi, [n - 1], n, U.attn_workers()[0], clusters=U.attn_clusters())
+            assert any(s[9] >= 0 for s in plan)
+        q = layer.queries(65 + seed)
+        want = torch.empty_like(q)
+        call(q, want, None)
+        work.append((call, q, torch.empty((calls,) + q.shape, dtype=q.dtype, device="cuda"), want))
+    torch.cuda.synchronize()
+
+    def body(call, q, outs, _):
+        for i in range(calls):
+            call(q, outs[i], PerThread)
+
+    for _ in range(2):
+        together(*(lambda w=w: body(*w) for w in work))           # threads that have ended leave the others' scratch alone
+    torch.cuda.synchronize()
+    for _, _, outs, want in work:
+        assert all(torch.equal(o.view(torch.int16), want.view(torch.int16)) for o in outs)
+    assert U.poll_status() == 0
