@@ -125,7 +125,8 @@ int unstep_rope_kv_append(const unstep_shape_t* shape, const int32_t* start_fram
  * buffer the library keeps per (device, stream).  The first call on a stream creates it with
  * cudaMalloc (two slots per SM, about 40 MB, whatever the problem): make that call outside any stream
  * capture.  Calls on one stream share the buffer safely, from whichever host threads they come; calls on
- * different streams use different buffers (cudaStreamPerThread is a stream of its own in every host thread).  Only the arrival counters depend on the problem: 8 bytes per work item (stream, head, pair
+ * different streams use different buffers (cudaStreamPerThread is a stream of its own in every host
+ * thread).  Only the arrival counters depend on the problem: 8 bytes per work item (stream, head, pair
  * of 128-query tiles; up to 32 streams), independent of the start frames and the window.  The first
  * call of a stream with more than 2048 work items, and any later one with more than there is room
  * for, gets a larger array (again by cudaMalloc, outside any capture); the former one is kept, and
@@ -301,13 +302,17 @@ int unstep_kv_read_q8(const unstep_shape_t* shape, int32_t sink_frames, const in
  *   q_rot, out : bf16 [B, L, Hn, 128].
  * Scratch: that of unstep_window_attn, shared with it; all it says about streams, captures and graphs holds here.  Where windows
  * are unpacked in front of the attention (more than 768 queries a stream, but for the smallest calls), as many heads at a time
- * as fit, that goes into a buffer of 16 to 256 MB per stream, made by the first call that needs that size and kept until
- * unstep_shutdown (smaller ones of former calls are kept too, for graphs).  Where it cannot be made - no memory left, or
- * inside a capture - the call decodes as it goes, which takes up to a third longer; a result may then differ in its last bits.
+ * as fit, that goes into a buffer of 16, 32, .. or 256 MB per stream, made by the first call that needs that size and kept until
+ * unstep_shutdown.  The smaller ones of former calls are kept too, for graphs: a stream that has gone through all sizes holds
+ * 496 MB.  Where the buffer cannot be made - no memory left, or inside a capture - and where the window of one head is larger
+ * than the largest (more than 524288 keys), the call decodes as it goes, which takes up to a third longer; a result may then
+ * differ in its last bits.  The launches of a call over unpacked windows are enqueued one behind the other: a call that
+ * another host thread makes on the stream meanwhile waits, on the host, until they are.
  *
  * unstep_window_attn_q8_way says how such a call is run on a device of `max_workers` SMs (unstep_attn_workers): *way (HOST) is 0
  * where keys go straight from the cache to the products (few queries, or few keys), 1 where tiles are decoded in the attention
- * kernel, 2 where windows are unpacked in front of it.  Host only, no GPU is needed: a diagnostic for tests and tuning.
+ * kernel, 2 where windows are unpacked in front of it, as far as there is a buffer for them (above; else the call is run as 1).
+ * Host only, no GPU is needed: a diagnostic for tests and tuning.
  */
 int unstep_window_attn_q8(const unstep_shape_t* shape, int32_t sink_frames, const int32_t* start_frame,
                           int32_t recent_frames, int32_t sink_attend, const void* q_rot, const void* cache_k,

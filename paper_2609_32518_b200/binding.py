@@ -531,7 +531,7 @@ def _general_window_attn_q8(shape, sink_frames, start_frame, recent_frames, sink
 def window_attn_q8_way(shape: Shape, sink_frames: int, start_frame, recent_frames: int, sink_attend: int,
                        max_workers: int) -> str:
     """unstep_window_attn_q8_way: how window_attn_q8 is run on a device of max_workers SMs: "few", "tiles" or
-    "unpacked".  Host only."""
+    "unpacked" (as "tiles" where the buffer for that cannot be made or does not hold the window of a head).  Host only."""
     way = c_int32(-1)
     _check(lib().unstep_window_attn_q8_way(ctypes.byref(shape), int(sink_frames), _starts(shape, start_frame),
                                            int(recent_frames), int(sink_attend), int(max_workers), ctypes.byref(way)),

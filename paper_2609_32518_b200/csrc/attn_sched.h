@@ -466,7 +466,8 @@ inline bool few_is_shorter(const AttnParams& p, const unstep_shape_t* shape, con
   return without < with;
 }
 
-// The way in which a call over an 8-bit cache is run (its first launch decides).
+// The way in which a call over an 8-bit cache is run (its first launch decides).  kUnpacked is what is wanted: without a
+// buffer that holds the window of a head (no memory, a capture, more than kMostWindow) the call is run as kTiles.
 enum Way { kFew, kTiles, kUnpacked };
 inline Way q8_way(const AttnParams& p, const unstep_shape_t* shape, const int32_t* start_frame, int32_t window_frames,
                   int32_t sink_attend, int32_t sm_count) {
