@@ -269,6 +269,10 @@ int unstep_rotary_apply(const unstep_shape_t* shape, const unstep_rope_t* rope, 
  * m <= 448 * 2^(E - 127), the code is x * 2^-(E - 127) rounded to e4m3 (nearest even), which is off by at most 2^-4 of the value
  * or 2^-10 * 2^(E - 127).  A block that holds a NaN, an infinity or a magnitude of 1.9375 * 2^127 or more has codes 0 and E = 255
  * and reads as NaN throughout.  What is read is exact in bf16, for every block that was written this way.
+ *
+ * The append writes neither of the two codes that are NaN in e4m3, 0x7F and 0xFF, and a cache that is filled by other means must not
+ * hold them in a frame that is read or attended: they are not looked for, and are decoded as +480 and -480 times the scale.
+ * (A conversion to e4m3 that does not saturate makes them of values beyond 448.)  NaN is a scale byte of 255.
  */
 
 /*
@@ -306,8 +310,8 @@ int unstep_kv_read_q8(const unstep_shape_t* shape, int32_t sink_frames, const in
  * unstep_shutdown.  The smaller ones of former calls are kept too, for graphs: a stream that has gone through all sizes holds
  * 496 MB.  Where the buffer cannot be made - no memory left, or inside a capture - and where the window of one head is larger
  * than the largest (more than 524288 keys), the call decodes as it goes, which takes up to a third longer; a result may then
- * differ in its last bits.  The launches of a call over unpacked windows are enqueued one behind the other: a call that
- * another host thread makes on the stream meanwhile waits, on the host, until they are.
+ * differ in its last bits.  The launches of a call over unpacked windows are enqueued one behind the other: another such
+ * call that a host thread makes on the stream meanwhile waits, on the host, until they are.
  *
  * unstep_window_attn_q8_way says how such a call is run on a device of `max_workers` SMs (unstep_attn_workers): *way (HOST) is 0
  * where keys go straight from the cache to the products (few queries, or few keys), 1 where tiles are decoded in the attention
@@ -347,6 +351,9 @@ int unstep_window_attn_q8_way(const unstep_shape_t* shape, int32_t sink_frames, 
  * Only the first launch of the call is listed (the first 32 streams).  Arguments are checked as in
  * unstep_window_attn_sink; sink_frames = 0 lists the plain rolling window.
  *
+ * Listed are the calls over a bf16 cache.  Those over an 8-bit cache go by the same rules where they have key tiles, but with key
+ * tiles and clusters of their own, and one launch for each group of heads that is unpacked.
+ *
  * With the workers and clusters of a device (the two functions below) the list is the launch on it.
  * unstep_window_attn_plan is the list for a device that runs no clusters.
  */
@@ -366,8 +373,8 @@ int unstep_window_attn_plan(const unstep_shape_t* shape, int32_t sink_frames, co
 int unstep_attn_workers(int32_t* workers, int32_t* ctas_per_worker);
 
 /*
- * The clusters of n attention thread blocks that the current device runs at the same time, n = 2 .. 8: the
- * `clusters` to give unstep_window_attn_plan_clusters.
+ * The clusters of n thread blocks of the attention over a bf16 cache that the current device runs at the same
+ * time, n = 2 .. 8: the `clusters` to give unstep_window_attn_plan_clusters.
  *   clusters : HOST int32 [9], written (0 in the first two).
  */
 int unstep_attn_clusters(int32_t* clusters);

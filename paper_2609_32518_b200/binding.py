@@ -568,7 +568,8 @@ def attn_workers():
 
 
 def attn_clusters():
-    """unstep_attn_clusters: how many clusters of n attention blocks run at the same time, at index n (2 .. 8)."""
+    """unstep_attn_clusters: how many clusters of n blocks of the attention over a bf16 cache run at the same time, at
+    index n (2 .. 8)."""
     buf = (c_int32 * 9)()
     _check(lib().unstep_attn_clusters(buf), "unstep_attn_clusters")
     return list(buf)

@@ -159,8 +159,10 @@ rotary_apply_kernel(const ApplyParams p, const uint4* x_in, const float4* cos_t,
 //
 // HBM bound without the norm: four streams of 4680 tokens x 12 heads (299 MB) 50.2 us, 6.0 TB/s, 0.91 of the measured copy rate.
 // With the norm a block's chain bounds it (loads, sum over
-// the block, gains, rotation, conversion; 4.7 long-scoreboard stalls an issue): one stream (75 MB) 20.1 us, 3.7 TB/s.  There
-// 10 blocks of 96 threads an SM 20.3, 8 21.3, 11 and 12 (spills) 22.6, 192 threads 22.9, 64 21.9; without the gains 16.0; the
+// the block, gains, rotation, conversion; 4.7 long-scoreboard stalls an issue): one stream (75 MB) 20.1 us, 3.7 TB/s.  Halves
+// behind the norm pass 8 floats for each vector of q and of k from lane to lane, and are the one form that spills: two heads a
+// thread have 64 registers (four blocks of 256 threads) and store 28 and load 48 bytes a thread.  There (halves)
+// 10 blocks of 96 threads an SM 20.3, 8 21.3, 11 and 12 (which spill more) 22.6, 192 threads 22.9, 64 21.9; without the gains 16.0; the
 // table's row in registers from the start, as without the norm, 22.3; v behind the sum 22.9.  Gains brought to shared memory
 // meanwhile: 19.3, but interleaved 18.4 instead of 17.8 and 10800 tokens 42.5 instead of 41.4; blocks that go through the
 // tokens with the next one's vectors on their way 34.  With four heads a thread at least two blocks an SM (128
@@ -537,6 +539,7 @@ extern "C" int unstep_rotary_kv_append_q8(const unstep_shape_t* shape, const uns
     // would not have the threads.  Halves / interleaved, 4680 tokens, us, one : two : three : four of them: 4 heads 5.8 / 5.0 :
     // 5.7 / 4.3 : 6.6 / 5.8 : 4.6 / 4.3, 7 9.4 / 8.6 : 9.2 / 7.8 : 10.2 / 9.4 : 8.5 / 8.3, 12 16.4 / 15.4 : 15.7 / 14.6 : 15.1 / 14.6 :
     // 17.8 / 17.7, 14 two 17.7 / 17.0, three 19.0 / 18.2, four 20.7 / 20.3, 20 24.8 / 22.6, 25.4 / 22.2 and 27.5 / 27.0.
+    // 40 heads three : four 46.4 / 40.2 : 43.4 / 42.7: the layouts differ there, and the rule goes by their sum.
     wide = shape->heads > 64;
     per_thread = shape->heads > 48 ? 4 : 3;
     auto places = [&](int u) { return (shape->heads + u - 1) / u * u; };
